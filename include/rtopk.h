@@ -57,7 +57,9 @@ enum {
   RTOPK_ERR_MISALIGNED = -5,    /* a pointer is not aligned to its element size */
   RTOPK_ERR_LAUNCH = -6,        /* the HIP runtime refused the launch */
   RTOPK_ERR_BAD_EPSILON = -7,   /* eps_rel is negative or NaN */
-  RTOPK_ERR_OVERLAP = -8        /* the input shares bytes with an output, or two outputs with each other */
+  RTOPK_ERR_OVERLAP = -8,       /* the input shares bytes with an output, or two outputs with each other */
+  RTOPK_ERR_BAD_TEMPERATURE = -9, /* a temperature that is not positive and finite, or whose reciprocal is not */
+  RTOPK_ERR_BAD_TYPE = -10      /* an element type that is none of RTOPK_F32, RTOPK_F16, RTOPK_BF16, or token_bytes neither 4 nor 8 */
 };
 
 /*
@@ -190,6 +192,88 @@ int rtopk_maxk_backward_gather(const float* grad_out, const int32_t* idx, int64_
                                float* grad_vals, void* stream);
 int rtopk_maxk_backward_gather_u8(const float* grad_out, const uint8_t* idx, int64_t N, int32_t M, int32_t k,
                                   float* grad_vals, void* stream);
+
+/*
+ * Operators on rows of logits
+ * ---------------------------
+ * A row x of M logits (fp32, half or bfloat16) at temperature T stands for the distribution q_v = exp(x_v / T - lse) with
+ * lse = ln sum_v exp(x_v / T).  All arithmetic is fp32 on the widened logits; a gradient is rounded once, to nearest even.  Logits may be
+ * -inf (masked columns); a row of nothing but -inf has lse -inf, entropy 0, log probabilities -inf and a gradient of zero.  A row with a NaN
+ * or +inf gives NaN results for itself (its alternatives' columns are then some columns of the row), and only for itself.
+ *
+ *   logits        : [N][M] of `dtype`, rows `stride` elements apart (stride >= M where N > 1; what lies between rows is not read),
+ *                   aligned to the element.  1 <= M <= rtopk_max_m().
+ *   dtype         : RTOPK_F32, RTOPK_F16 or RTOPK_BF16.
+ *   temperature   : > 0, finite, as is its reciprocal (RTOPK_ERR_BAD_TEMPERATURE otherwise).
+ *   workspace     : with at least rtopk_logits_workspace_bytes(...) bytes of device memory (16-byte aligned, sharing no byte with the other
+ *                   buffers) few wide rows are spread over several workgroups each, in two launches (three where a gradient takes its
+ *                   logits' place) instead of one; the memory may be used again by later work on that stream.  Without it (NULL, too few
+ *                   bytes, or a shape for which that function returns 0) a row is one workgroup's work.  The results of both differ by rounding only.
+ *   Outputs may be NULL where marked (optional).  Results do not depend on what else runs: no sum is taken in an order of chance.
+ */
+enum { RTOPK_F32 = 0, RTOPK_F16 = 1, RTOPK_BF16 = 2 };
+
+/* Device memory for the calls below that take some; k: alternatives of rtopk_token_logprobs, 0 for the others. */
+int64_t rtopk_logits_workspace_bytes(int64_t N, int32_t M, int32_t dtype, int32_t k);
+
+/*
+ * Log probabilities of given tokens, entropy and top alternatives; every logit is read once.
+ *   tokens           : [N][G] columns, int32_t or int64_t (token_bytes 4 or 8), 0 <= G <= 1024 (NULL where G is 0).  A token outside [0, M)
+ *                      is left out: its log probability is written as 0.
+ *   k                : alternatives of each row, 0 <= k <= min(128, M).
+ *   out_logprobs     : [N][G] fp32, ln q at the tokens (NULL where G is 0).
+ *   out_entropy      : [N] fp32, -sum_v q_v ln q_v (optional).
+ *   out_lse          : [N] fp32 (optional); the backward call takes it.
+ *   out_top_logprobs : [N][k] fp32, ln q of the k largest logits, largest first; equal logits by ascending column (NULL where k is 0).
+ *   out_top_cols     : [N][k] int32_t, their columns (NULL where k is 0).
+ */
+int rtopk_token_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride, const void* tokens, int32_t token_bytes,
+                         int32_t G, int32_t k, float temperature, float* out_logprobs, float* out_entropy, float* out_lse,
+                         float* out_top_logprobs, int32_t* out_top_cols, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of the above with respect to the logits,
+ *   (1 / T) (sum_g grad_logprobs_g (1[v == token_g] - q_v) - grad_entropy q_v (ln q_v + entropy)),
+ * one launch; logits read once, gradient written once.  Rows whose tokens' gradients sum to zero (tokens left out have none) and whose entropy
+ * has no gradient are not read.
+ *   grad_logprobs : [N][G] fp32 (NULL where G is 0).      grad_entropy : [N] fp32, or NULL: the entropy has no gradient.
+ *   lse           : [N] fp32 as the forward call wrote it at the same temperature.   entropy : [N] fp32 likewise (with grad_entropy only).
+ *   grad_logits   : [N][M] of `dtype`, rows grad_stride >= M apart.  It may be the logits themselves (same address and stride), which it then
+ *                   replaces; any other overlap is RTOPK_ERR_OVERLAP.
+ */
+int rtopk_token_logprobs_backward(const float* grad_logprobs, const float* grad_entropy, const void* logits, int32_t dtype, int64_t N, int32_t M,
+                                  int64_t stride, const void* tokens, int32_t token_bytes, int32_t G, const float* lse, const float* entropy,
+                                  float temperature, void* grad_logits, int64_t grad_stride, void* stream);
+
+/*
+ * Distillation from a teacher's top logits: loss_n = sum_j p_j (ln p_j - ln q_{c_j}) over the row's k entries (t_j, c_j), with
+ * p = softmax(t / T) over the entries that count, or p_j = exp(t_j) where log_probs is 1 (t are then log probabilities at the temperature, as
+ * rtopk_token_logprobs writes them; what mass the list lacks adds nothing).  The pairs may be those of rtopk_rowwise* or of
+ * rtopk_token_logprobs, in any order.  An entry whose column is outside [0, M), or whose value is -inf, does not count; a row without
+ * any has loss 0 and gradient 0.  Entries with the same column add up.
+ *   teacher_vals : [N][k] of teacher_dtype; teacher_cols : [N][k] int32_t; 1 <= k <= 1024.
+ *   out_loss     : [N] fp32.      out_lse : [N] fp32 (optional); the backward call takes it.
+ */
+int rtopk_distill(const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride, const void* teacher_vals, int32_t teacher_dtype,
+                  const int32_t* teacher_cols, int32_t k, int32_t log_probs, float temperature, float* out_loss, float* out_lse,
+                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * grad_loss_n dloss_n / dx_v = (grad_loss_n / T) (q_v sum_j p_j - sum_{j: c_j == v} p_j), one launch.  lse, grad_logits: as for
+ * rtopk_token_logprobs_backward.  Rows without a gradient (grad_loss 0, or no entry that counts) are not read.
+ */
+int rtopk_distill_backward(const float* grad_loss, const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride,
+                           const void* teacher_vals, int32_t teacher_dtype, const int32_t* teacher_cols, int32_t k, int32_t log_probs,
+                           const float* lse, float temperature, void* grad_logits, int64_t grad_stride, void* stream);
+
+/*
+ * Both at once, for weights [N] that are known before the loss is (1 / N for a mean): out_loss as rtopk_distill's, not weighted, grad_logits as
+ * rtopk_distill_backward's for grad_loss = weights.  Rows without an entry that counts are not read.
+ */
+int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride,
+                            const void* teacher_vals, int32_t teacher_dtype, const int32_t* teacher_cols, int32_t k, int32_t log_probs,
+                            float temperature, float* out_loss, void* grad_logits, int64_t grad_stride, void* workspace,
+                            int64_t workspace_bytes, void* stream);
 
 /* Human-readable text for a status code (static storage, never NULL). */
 const char* rtopk_status_string(int status);

@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kVersion = 700;  // 0.7.0
+constexpr int kVersion = 800;  // 0.8.0
 
 inline uintptr_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 inline bool aligned(const void* p, uintptr_t a) { return rtopk::is_aligned(addr(p), a); }
@@ -264,6 +264,8 @@ const char* rtopk_status_string(int status) {
     case RTOPK_ERR_LAUNCH: return "the HIP runtime refused the launch";
     case RTOPK_ERR_BAD_EPSILON: return "eps_rel must be >= 0";
     case RTOPK_ERR_OVERLAP: return "input and output buffers overlap";
+    case RTOPK_ERR_BAD_TEMPERATURE: return "temperature must be positive and finite, and so must its reciprocal";
+    case RTOPK_ERR_BAD_TYPE: return "unknown element type, or tokens of neither 4 nor 8 bytes";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,67 @@
+// Operators on rows of logits: limits, and how a call's rows are laid over workgroups.  Host code only (no HIP headers), so that a CPU
+// test can sweep the rules.
+#pragma once
+
+#include <stdint.h>
+
+namespace rtopk {
+
+constexpr int kMaxLogitsM = 1 << 24;  // widest row
+constexpr int kMaxAlternatives = 128; // top alternatives of a row
+constexpr int kMaxList = 1024;        // given tokens of a row, entries of a teacher's list
+constexpr int kMaxLogitsSegments = 256;     // workgroups that a row is spread over
+constexpr int kMaxMergeKeys = 2048;   // alternatives of all segments of a row that are merged
+
+// Columns of a 128-bit load.
+constexpr int logits_width(int dtype) { return dtype == 0 ? 4 : 8; }
+
+// A row over `segments` workgroups of `waves` wavefronts, `cols` columns each (the last one what is left); cols is a multiple of the load's.
+struct LogitsLayout {
+  int waves, segments, cols;
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A workgroup for each row.
+inline LogitsLayout logits_layout_whole(int64_t N, int M, int k) {
+  return {M <= 2048 && k <= 32 ? 1 : (N <= 256 ? 16 : 4), 1, M};
+}
+
+inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
+  const int v = logits_width(dtype);
+  const int64_t bytes = (int64_t)M * (dtype == 0 ? 4 : 2);
+  int64_t segments = 1;
+  if (N < 512) {
+    segments = ceil_div(1024, N);
+    if (segments > ceil_div(bytes, 16384)) segments = ceil_div(bytes, 16384);
+  }
+  if (segments > kMaxLogitsSegments) segments = kMaxLogitsSegments;
+  if (k > 0 && segments * k > kMaxMergeKeys) segments = kMaxMergeKeys / k;
+  LogitsLayout l;
+  l.cols = (int)(ceil_div(ceil_div(M, segments), v) * v);
+  l.segments = (int)ceil_div(M, l.cols);
+  l.waves = 4;
+  return l.segments > 1 ? l : logits_layout_whole(N, M, k);
+}
+
+// The segments of a gradient whose row sums are known.  A gradient that takes its logits' place has one: a row whose log-sum-exp is large is
+// read whole before any of it is written.
+inline LogitsLayout logits_grad_layout(int64_t N, int M, int dtype, bool in_place) {
+  if (in_place) return {4, 1, M};
+  const int v = logits_width(dtype);
+  int64_t cols = 32768 / (dtype == 0 ? 4 : 2);
+  while (cols > 1024 * v / 4 && N * ceil_div(M, cols) < 1024) cols /= 2;
+  LogitsLayout l;
+  l.segments = (int)ceil_div(M, cols);
+  l.cols = (int)(ceil_div(ceil_div(M, l.segments), v) * v);
+  l.segments = (int)ceil_div(M, l.cols);
+  l.waves = 4;
+  return l;
+}
+
+// Device memory for the segments' partial results: maximum, sum and weighted sum of each, then its alternatives.
+inline int64_t logits_workspace(int64_t N, const LogitsLayout& l, int k) {
+  return l.segments > 1 ? N * l.segments * (16 + 8 * (int64_t)k) : 0;
+}
+
+}  // namespace rtopk

@@ -313,6 +313,248 @@ PyObject* gather(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- operators on rows of logits ----
+
+// Rows of logits (or their gradient): a matrix whose rows are contiguous, any distance apart that keeps them from overlapping.
+struct Rows {
+  void* data = nullptr;
+  int64_t N = 0, stride = 0;
+  int32_t M = 0, dtype = 0;
+  at::ScalarType type = at::kFloat;
+  bool set(const Tensor* t) {
+    if (!t || !t->is_cuda() || t->dim() != 2 || t->size(1) > std::numeric_limits<int32_t>::max()) return false;
+    type = t->scalar_type();
+    if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return false;
+    dtype = type == at::kFloat ? RTOPK_F32 : (type == at::kHalf ? RTOPK_F16 : RTOPK_BF16);
+    N = t->size(0);
+    M = (int32_t)t->size(1);
+    stride = N > 1 ? t->stride(0) : M;
+    data = t->data_ptr();
+    return (t->stride(1) == 1 || M <= 1) && stride >= M;
+  }
+};
+
+bool is_vector(const Tensor* t, at::ScalarType type, int64_t n, c10::Device device) {
+  return t && t->device() == device && t->scalar_type() == type && t->dim() == 1 && t->size(0) == n && t->is_contiguous();
+}
+
+// Given tokens: [N] or [N, G], 32 or 64 bits.
+struct Tokens {
+  const void* data = nullptr;
+  int32_t bytes = 0, G = 1;
+  bool set(const Tensor* t, int64_t N, c10::Device device) {
+    if (!t || t->device() != device || !t->is_contiguous() || t->dim() < 1 || t->dim() > 2 || t->size(0) != N) return false;
+    if (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong) return false;
+    if (t->dim() == 2 && t->size(1) > 1024) return false;
+    bytes = t->scalar_type() == at::kLong ? 8 : 4;
+    G = t->dim() == 2 ? (int32_t)t->size(1) : 1;
+    data = t->data_ptr();
+    return true;
+  }
+};
+
+// The teacher's list: values and columns [N, k].
+struct Teacher {
+  const void* vals = nullptr;
+  const int32_t* cols = nullptr;
+  int32_t dtype = 0, k = 0, log_probs = 0;
+  bool set(PyObject* v, PyObject* c, PyObject* lp, int64_t N, c10::Device device) {
+    Rows r;
+    const Tensor *tv = tensor_of(v), *tc = tensor_of(c);
+    if (!r.set(tv) || !tv->is_contiguous() || r.N != N || tv->device() != device) return false;
+    if (!tc || tc->device() != device || !is_shape(*tc, at::kInt, N, r.M)) return false;
+    const int truth = PyObject_IsTrue(lp);
+    if (truth < 0) {
+      PyErr_Clear();
+      return false;
+    }
+    vals = r.data;
+    cols = static_cast<const int32_t*>(tc->data_ptr());
+    dtype = r.dtype;
+    k = r.M;
+    log_probs = truth;
+    return true;
+  }
+};
+
+// Scratch memory as above.
+struct LogitsScratch {
+  Tensor tensor;
+  void* data = nullptr;
+  int64_t bytes = 0;
+  LogitsScratch(const Tensor& x, const Rows& r, int32_t k, bool plain) {
+    bytes = rtopk_logits_workspace_bytes(r.N, r.M, r.dtype, k);
+    if (bytes > 0) {
+      try {
+        tensor = new_tensor({bytes}, at::kByte, x.device(), plain);
+        data = tensor.data_ptr();
+      } catch (const c10::OutOfMemoryError&) {
+        bytes = 0;
+      }
+    }
+  }
+};
+
+// The gradient: the caller's rows, or new ones.
+struct Gradient {
+  Output made;
+  Rows rows;
+  bool set(PyObject* given, const Tensor& x, const Rows& r, bool plain) {
+    if (given != Py_None) {
+      const Tensor* t = tensor_of(given);
+      if (!rows.set(t) || t->device() != x.device() || rows.type != r.type || rows.N != r.N || rows.M != r.M) return false;
+      made.object = Py_NewRef(given);
+      return true;
+    }
+    return made.set(Py_None, r.type, {r.N, (int64_t)r.M}, x.device(), plain) && rows.set(&made.tensor);
+  }
+};
+
+template <typename... O>
+PyObject* tuple_of(O&... outputs) {
+  PyObject* t = PyTuple_New(sizeof...(outputs));
+  if (!t) return nullptr;
+  Py_ssize_t i = 0;
+  (PyTuple_SET_ITEM(t, i++, outputs.release()), ...);
+  return t;
+}
+
+PyObject* failed() { return PyErr_Occurred() ? nullptr : none(); }
+
+float* floats(Output& o) { return static_cast<float*>(o.tensor.data_ptr()); }
+
+// token_logprobs(logits, tokens, k, temperature, out_logprobs, out_entropy, out_lse, out_top_logprobs, out_top_cols)
+PyObject* token_logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    int32_t k;
+    float temperature;
+    const Tensor* x = n == 9 ? tensor_of(args[0]) : nullptr;
+    const Tensor* given = x ? tensor_of(args[1]) : nullptr;
+    Rows r;
+    Tokens t;
+    if (!r.set(x) || !t.set(given, r.N, x->device()) || !int32_of(args[2], k) || k < 0 || !float_of(args[3], temperature)) return none();
+    if (k == 0 && (args[7] != Py_None || args[8] != Py_None)) return none();
+    const bool plain = is_plain();
+    Output lp, h, lse, tl, tc;
+    if (!lp.set(args[4], at::kFloat, given->sizes(), x->device(), plain) || !h.set(args[5], at::kFloat, {r.N}, x->device(), plain) ||
+        !lse.set(args[6], at::kFloat, {r.N}, x->device(), plain))
+      return failed();
+    if (k > 0 && (!tl.set(args[7], at::kFloat, {r.N, k}, x->device(), plain) || !tc.set(args[8], at::kInt, {r.N, k}, x->device(), plain)))
+      return failed();
+    float *p_lp = floats(lp), *p_h = floats(h), *p_lse = floats(lse), *p_tl = k > 0 ? floats(tl) : nullptr;
+    int32_t* p_tc = k > 0 ? static_cast<int32_t*>(tc.tensor.data_ptr()) : nullptr;
+    void* s = stream_of(*x);
+    LogitsScratch w(*x, r, k, plain);
+    const int status = unlocked([&] {
+      return rtopk_token_logprobs(r.data, r.dtype, r.N, r.M, r.stride, t.data, t.bytes, t.G, k, temperature, p_lp, p_h, p_lse, p_tl, p_tc, w.data,
+                                  w.bytes, s);
+    });
+    if (status != RTOPK_OK) return none();
+    return k > 0 ? tuple_of(lp, h, lse, tl, tc) : tuple_of(lp, h, lse);
+  });
+}
+
+// token_logprobs_backward(grad_logprobs, logits, tokens, lse, temperature, grad_entropy, entropy, grad_logits)
+PyObject* token_logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float temperature;
+    const Tensor* x = n == 8 ? tensor_of(args[1]) : nullptr;
+    const Tensor* given = x ? tensor_of(args[2]) : nullptr;
+    Rows r;
+    Tokens t;
+    if (!r.set(x) || !t.set(given, r.N, x->device()) || !float_of(args[4], temperature)) return none();
+    const Tensor *g = tensor_of(args[0]), *lse = tensor_of(args[3]);
+    if (!g || g->device() != x->device() || g->scalar_type() != at::kFloat || !g->is_contiguous() || g->sizes() != given->sizes()) return none();
+    if (!is_vector(lse, at::kFloat, r.N, x->device())) return none();
+    const float *p_gh = nullptr, *p_h = nullptr;
+    if (args[5] != Py_None) {
+      const Tensor *gh = tensor_of(args[5]), *h = tensor_of(args[6]);
+      if (!is_vector(gh, at::kFloat, r.N, x->device()) || !is_vector(h, at::kFloat, r.N, x->device())) return none();
+      p_gh = static_cast<const float*>(gh->data_ptr());
+      p_h = static_cast<const float*>(h->data_ptr());
+    }
+    Gradient d;
+    if (!d.set(args[7], *x, r, is_plain())) return failed();
+    const float *p_g = static_cast<const float*>(g->data_ptr()), *p_lse = static_cast<const float*>(lse->data_ptr());
+    void* s = stream_of(*x);
+    const int status = unlocked([&] {
+      return rtopk_token_logprobs_backward(p_g, p_gh, r.data, r.dtype, r.N, r.M, r.stride, t.data, t.bytes, t.G, p_lse, p_h, temperature,
+                                           d.rows.data, d.rows.stride, s);
+    });
+    return status == RTOPK_OK ? d.made.release() : none();
+  });
+}
+
+// distill(logits, teacher_vals, teacher_cols, temperature, log_probs, out_loss, out_lse)
+PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float temperature;
+    const Tensor* x = n == 7 ? tensor_of(args[0]) : nullptr;
+    Rows r;
+    Teacher t;
+    if (!r.set(x) || !float_of(args[3], temperature) || !t.set(args[1], args[2], args[4], r.N, x->device())) return none();
+    const bool plain = is_plain();
+    Output loss, lse;
+    if (!loss.set(args[5], at::kFloat, {r.N}, x->device(), plain) || !lse.set(args[6], at::kFloat, {r.N}, x->device(), plain)) return failed();
+    float *p_loss = floats(loss), *p_lse = floats(lse);
+    void* s = stream_of(*x);
+    LogitsScratch w(*x, r, 0, plain);
+    const int status = unlocked([&] {
+      return rtopk_distill(r.data, r.dtype, r.N, r.M, r.stride, t.vals, t.dtype, t.cols, t.k, t.log_probs, temperature, p_loss, p_lse, w.data,
+                           w.bytes, s);
+    });
+    return status == RTOPK_OK ? tuple_of(loss, lse) : none();
+  });
+}
+
+// distill_backward(grad_loss, logits, teacher_vals, teacher_cols, lse, temperature, log_probs, grad_logits)
+PyObject* distill_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float temperature;
+    const Tensor* x = n == 8 ? tensor_of(args[1]) : nullptr;
+    Rows r;
+    Teacher t;
+    if (!r.set(x) || !float_of(args[5], temperature) || !t.set(args[2], args[3], args[6], r.N, x->device())) return none();
+    const Tensor *g = tensor_of(args[0]), *lse = tensor_of(args[4]);
+    if (!is_vector(g, at::kFloat, r.N, x->device()) || !is_vector(lse, at::kFloat, r.N, x->device())) return none();
+    Gradient d;
+    if (!d.set(args[7], *x, r, is_plain())) return failed();
+    const float *p_g = static_cast<const float*>(g->data_ptr()), *p_lse = static_cast<const float*>(lse->data_ptr());
+    void* s = stream_of(*x);
+    const int status = unlocked([&] {
+      return rtopk_distill_backward(p_g, r.data, r.dtype, r.N, r.M, r.stride, t.vals, t.dtype, t.cols, t.k, t.log_probs, p_lse, temperature,
+                                    d.rows.data, d.rows.stride, s);
+    });
+    return status == RTOPK_OK ? d.made.release() : none();
+  });
+}
+
+// distill_with_grad(weights, logits, teacher_vals, teacher_cols, temperature, log_probs, out_loss, grad_logits)
+PyObject* distill_with_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float temperature;
+    const Tensor* x = n == 8 ? tensor_of(args[1]) : nullptr;
+    Rows r;
+    Teacher t;
+    if (!r.set(x) || !float_of(args[4], temperature) || !t.set(args[2], args[3], args[5], r.N, x->device())) return none();
+    const Tensor* g = tensor_of(args[0]);
+    if (!is_vector(g, at::kFloat, r.N, x->device())) return none();
+    const bool plain = is_plain();
+    Output loss;
+    Gradient d;
+    if (!loss.set(args[6], at::kFloat, {r.N}, x->device(), plain) || !d.set(args[7], *x, r, plain)) return failed();
+    const float* p_g = static_cast<const float*>(g->data_ptr());
+    float* p_loss = floats(loss);
+    void* s = stream_of(*x);
+    LogitsScratch w(*x, r, 0, plain);
+    const int status = unlocked([&] {
+      return rtopk_distill_with_grad(p_g, r.data, r.dtype, r.N, r.M, r.stride, t.vals, t.dtype, t.cols, t.k, t.log_probs, temperature, p_loss,
+                                     d.rows.data, d.rows.stride, w.data, w.bytes, s);
+    });
+    return status == RTOPK_OK ? tuple_of(loss, d.made) : none();
+  });
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -321,7 +563,10 @@ PyCFunction fast(F f) {
 PyMethodDef kMethods[] = {
     {"select", fast(select), METH_FASTCALL, nullptr},   {"select_eps", fast(select_eps), METH_FASTCALL, nullptr},
     {"dense", fast(dense), METH_FASTCALL, nullptr},     {"scatter", fast(scatter), METH_FASTCALL, nullptr},
-    {"gather", fast(gather), METH_FASTCALL, nullptr},   {nullptr, nullptr, 0, nullptr},
+    {"gather", fast(gather), METH_FASTCALL, nullptr},   {"token_logprobs", fast(token_logprobs), METH_FASTCALL, nullptr},
+    {"token_logprobs_backward", fast(token_logprobs_backward), METH_FASTCALL, nullptr},
+    {"distill", fast(distill), METH_FASTCALL, nullptr}, {"distill_backward", fast(distill_backward), METH_FASTCALL, nullptr},
+    {"distill_with_grad", fast(distill_with_grad), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
 };
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_rtopk_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -60,6 +60,19 @@ def load_library() -> ctypes.CDLL:
             getattr(lib, name).restype = ctypes.c_int
         lib.rtopk_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
         lib.rtopk_workspace_bytes.restype = i64
+        f32 = ctypes.c_float
+        rows = [vp, i32, i64, i32, i64]  # logits, dtype, N, M, stride
+        teacher = [vp, i32, vp, i32, i32]  # teacher_vals, teacher_dtype, teacher_cols, k, log_probs
+        lib.rtopk_logits_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        lib.rtopk_logits_workspace_bytes.restype = i64
+        lib.rtopk_token_logprobs.argtypes = [*rows, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+        lib.rtopk_token_logprobs_backward.argtypes = [vp, vp, *rows, vp, i32, i32, vp, vp, f32, vp, i64, vp]
+        lib.rtopk_distill.argtypes = [*rows, *teacher, f32, vp, vp, vp, i64, vp]
+        lib.rtopk_distill_backward.argtypes = [vp, *rows, *teacher, vp, f32, vp, i64, vp]
+        lib.rtopk_distill_with_grad.argtypes = [vp, *rows, *teacher, f32, vp, vp, i64, vp, i64, vp]
+        for name in ("rtopk_token_logprobs", "rtopk_token_logprobs_backward", "rtopk_distill", "rtopk_distill_backward",
+                     "rtopk_distill_with_grad"):
+            getattr(lib, name).restype = ctypes.c_int
         lib.rtopk_status_string.argtypes = [ctypes.c_int]
         lib.rtopk_status_string.restype = ctypes.c_char_p
         _lib = lib
