@@ -52,6 +52,23 @@ struct Logits {
     else if constexpr (DT == kBF16) return __uint_as_float((c & 1) ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[c / 2] >> (16 * (c & 1))));
   }
+  // the largest of a load
+  static __device__ __forceinline__ float largest(const u4_vec& w) {
+    if constexpr (DT == kF16) {
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+      const auto two = [&](int i) {
+        const uint32_t v = w[i];  // (a bit cast of the element itself takes element 0)
+        return __builtin_bit_cast(h2, v);
+      };
+      const h2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(0), two(1)), __builtin_elementwise_max(two(2), two(3)));
+      return vmax((float)m[0], (float)m[1]);
+    } else {
+      float m = vmax(at(w, 0), at(w, 1));
+#pragma unroll
+      for (int i = 2; i < V; i += 2) m = vmax3(m, at(w, i), at(w, i + 1));
+      return m;
+    }
+  }
   static __device__ __forceinline__ elem narrow(float v) {  // to nearest even
     if constexpr (DT == kF32) return v;
     else if constexpr (DT == kBF16) return __builtin_bit_cast(uint16_t, (__bf16)v);
@@ -73,10 +90,11 @@ struct Logits {
 
 // ---- order of the alternatives --------------------------------------------------------------------
 
-// A whole number in the order of the logits; -0 and +0 are equal, NaN is above all; 0 stands for no logit.
+// A whole number in the order of the logits; -0 and +0 are equal, NaN counts as -inf; 0 stands for no logit.
+constexpr uint32_t kLowKey = 0x007fffffu;  // of -inf
 __device__ __forceinline__ uint32_t order_key(float v) {
+  if (!(v > kNegInf)) return kLowKey;
   const uint32_t b = __float_as_uint(v + 0.0f);
-  if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t key) {
@@ -88,20 +106,30 @@ __device__ __forceinline__ int place_col(uint64_t key) { return (int)~(uint32_t)
 
 // ---- sums -----------------------------------------------------------------------------------------
 
+// Of the 64 lanes, in every lane, in a fixed order: within 16 lanes by DPP permutations, then across them to lane 63.
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, float none, F f) {
+  const auto moved = [&](auto ctrl, auto rows) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using all = std::integral_constant<int, 0xf>;
+  v = f(v, moved(std::integral_constant<int, 0xb1>{}, all{}));                                  // quad_perm [1, 0, 3, 2]
+  v = f(v, moved(std::integral_constant<int, 0x4e>{}, all{}));                                  // quad_perm [2, 3, 0, 1]
+  v = f(v, moved(std::integral_constant<int, 0x141>{}, all{}));                                 // row_half_mirror
+  v = f(v, moved(std::integral_constant<int, 0x140>{}, all{}));                                 // row_mirror
+  v = f(v, moved(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));    // row_bcast:15
+  v = f(v, moved(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));    // row_bcast:31
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return wave_reduce(v, kNegInf, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
 }
 
 struct Stats {
-  float m, s, a;  // maximum, S and A about it (0 where the maximum is -inf)
-  __device__ __forceinline__ float about() const { return m == kNegInf ? 0.0f : m; }
+  float m, s, a;  // maximum, S and A about it
 };
 
 // The factor and the sums of `t` about a maximum that is no smaller; c = log2(e) / T.
@@ -114,141 +142,251 @@ __device__ __forceinline__ void scale_to(Stats& t, float m, float c) {
   t.m = m;
 }
 
+// While a row is read the sums are about r = m c, rounded, in powers of two: one fused multiply-add and one exp2 to a logit, and the rounding of r
+// is in all terms alike.  s = sum 2^(x c - r), a = sum 2^(x c - r) (x c - r).
+struct Running {
+  float m, s, a;
+};
+__device__ __forceinline__ float reference(float m, float c) { return fmaxf(m * c, -1e37f); }
+
 template <bool ENT>
-__device__ __forceinline__ Stats wave_join(Stats t, float c) {
-  scale_to<ENT>(t, wave_max(t.m), c);
-  t.s = wave_sum(t.s);
-  if (ENT) t.a = wave_sum(t.a);
-  return t;
+__device__ __forceinline__ void rise_to(Running& t, float m, float c) {
+  const float d = reference(t.m, c) - reference(m, c), f = __builtin_amdgcn_exp2f(d);
+  if (ENT) t.a = f * __builtin_fmaf(t.s, fmaxf(d, kFar), t.a);
+  t.s *= f;
+  t.m = m;
 }
 
 // All W wavefronts' sums, in every thread.  `room`: W entries; a barrier lies between its writes and reads.
 template <int W, bool ENT>
-__device__ __forceinline__ Stats block_join(Stats t, float c, float4* room) {
-  t = wave_join<ENT>(t, c);
+__device__ __forceinline__ Running block_join(Running t, float c, float4* room) {
+  rise_to<ENT>(t, wave_max(t.m), c);
+  t.s = wave_sum(t.s);
+  if (ENT) t.a = wave_sum(t.a);
   if (W == 1) return t;
   if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = make_float4(t.m, t.s, t.a, 0.0f);
   __syncthreads();
   float m = room[0].x;
 #pragma unroll
   for (int w = 1; w < W; ++w) m = fmaxf(m, room[w].x);
-  Stats all = {m, 0.0f, 0.0f};
+  Running all = {m, 0.0f, 0.0f};
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    Stats u = {room[w].x, room[w].y, room[w].z};
-    scale_to<ENT>(u, m, c);
+    Running u = {room[w].x, room[w].y, room[w].z};
+    rise_to<ENT>(u, m, c);
     all.s += u.s;
     all.a += u.a;
   }
   return all;
 }
 
-// Takes U loads into a thread's sums.
-template <int DT, int U, bool ENT>
-__device__ __forceinline__ void absorb(const u4_vec (&w)[U], float c, Stats& t) {
-  using L = Logits<DT>;
-  float x[U * L::V];
+// Behind the main path: what seldom follows widens the loads again, rather than that every value is kept for it.
+template <int U>
+__device__ __forceinline__ void apart(u4_vec (&w)[U]) {
 #pragma unroll
-  for (int i = 0; i < U * L::V; ++i) x[i] = L::at(w[i / L::V], i % L::V);
+  for (int u = 0; u < U; ++u) asm volatile("" : "+v"(w[u]));
+}
+
+// Takes U loads into a thread's sums; top: their maxima.  MASKED: -inf is to be expected.
+template <int DT, int U, bool ENT, bool MASKED>
+__device__ __forceinline__ void absorb(u4_vec (&w)[U], float c, Running& t, float (&top)[U]) {
+  using L = Logits<DT>;
   float m = t.m;
 #pragma unroll
-  for (int i = 0; i < U * L::V; i += 2) m = vmax3(m, x[i], x[i + 1]);
-  scale_to<ENT>(t, m, c);
-  const float about = t.about();
-  float s[2] = {t.s, 0.0f}, a[2] = {t.a, 0.0f};
+  for (int u = 0; u < U; ++u) top[u] = L::largest(w[u]);
+#pragma unroll
+  for (int u = 0; u + 1 < U; u += 2) m = vmax3(m, top[u], top[u + 1]);
+  if (U % 2 != 0) m = vmax(m, top[U - 1]);
+  rise_to<ENT>(t, m, c);
+  const float r = reference(t.m, c);
+  float s[2] = {0.0f, 0.0f}, a[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < U * L::V; ++i) {
-    const float d = x[i] - about, e = __builtin_amdgcn_exp2f(d * c);
+    const float y = __builtin_fmaf(L::at(w[i / L::V], i % L::V), c, -r), e = __builtin_amdgcn_exp2f(y);
     s[i & 1] += e;
-    if (ENT) a[i & 1] = __builtin_fmaf(e, fmaxf(d, kFar), a[i & 1]);
+    if (ENT) a[i & 1] = __builtin_fmaf(e, MASKED ? fmaxf(y, kFar) : y, a[i & 1]);
   }
-  t.s = s[0] + s[1];
-  t.a = a[0] + a[1];
+  t.s += s[0] + s[1];
+  apart(w);
+  if (ENT) {
+    if (!MASKED && !(a[0] + a[1] == a[0] + a[1])) {  // 0 times -inf, from masked columns
+      a[0] = a[1] = 0.0f;
+      float again = r;
+      asm volatile("" : "+v"(again));
+#pragma unroll
+      for (int i = 0; i < U * L::V; ++i) {
+        const float y = __builtin_fmaf(L::at(w[i / L::V], i % L::V), c, -again);
+        a[i & 1] = __builtin_fmaf(__builtin_amdgcn_exp2f(y), fmaxf(y, kFar), a[i & 1]);
+      }
+    }
+    t.a += a[0] + a[1];
+  }
 }
 
 // ---- a thread's share of a segment ----------------------------------------------------------------
 
-// `cols` columns from `row` on, in chunks of a load's width; chunk i belongs to thread i mod T, the last one may be partial.
+// `cols` columns from `row` on, in chunks of a load's width; chunk i belongs to thread i mod T.  Rows of 16-bit values that start at an odd one
+// have their first column (`lead`) apart, so that all loads start at multiples of four bytes: from there they run at the rate of aligned ones
+// (8191 x 50001 half: 174 -> 135 us).  What is left at the end (`rest`, less than a chunk) and the lead make up the last chunk.
 template <int DT>
 struct Segment {
   using L = Logits<DT>;
-  const typename L::elem* row;
-  int full, rest;  // whole chunks, columns beyond them
-  __device__ __forceinline__ Segment(const typename L::elem* r, int cols) : row(r), full(cols / L::V), rest(cols % L::V) {}
-  __device__ __forceinline__ int chunks() const { return full + (rest != 0); }
-  // chunk `i` (i < chunks()), -inf past the end
+  const typename L::elem* body;  // of the whole chunks
+  int lead, full, rest;
+  __device__ __forceinline__ Segment(const typename L::elem* row, int cols) {
+    lead = DT == kF32 ? 0 : (int)((reinterpret_cast<uintptr_t>(row) >> 1) & 1);
+    body = row + lead;
+    full = (cols - lead) / L::V;
+    rest = (cols - lead) % L::V;
+  }
+  __device__ __forceinline__ int chunks() const { return full + (rest + lead != 0); }
+  // the last chunk: the rest's columns first, the lead in the last place, -inf between
   __device__ __forceinline__ u4_vec partial() const {
-    u4_vec w = {L::kLow, L::kLow, L::kLow, L::kLow};
-    const typename L::elem* p = row + (int64_t)full * L::V;
+    const int end = full * L::V;
+    typename L::elem v[L::V];  // (loaded without a branch, so together)
 #pragma unroll
-    for (int c = 0; c < L::V - 1; ++c)
-      if (c < rest) {
-        if constexpr (DT == kF32) w[c] = __float_as_uint(p[c]);
-        else w[c / 2] = (c & 1) ? (w[c / 2] & 0xffffu) | (uint32_t)p[c] << 16 : (w[c / 2] & 0xffff0000u) | p[c];
-      }
+    for (int c = 0; c < L::V; ++c) v[c] = body[c < rest ? end + c : (lead != 0 ? -1 : end)];
+    u4_vec w;
+#pragma unroll
+    for (int c = 0; c < L::V; ++c) {
+      const bool is = c < rest || (c == L::V - 1 && lead != 0);
+      if constexpr (DT == kF32) w[c] = is ? __float_as_uint(v[c]) : L::kLow;
+      else if ((c & 1) == 0) w[c / 2] = is ? v[c] : L::kLow & 0xffffu;
+      else w[c / 2] |= (is ? (uint32_t)v[c] : L::kLow & 0xffffu) << 16;
+    }
     return w;
   }
   // f(columns from the segment's start, value) for each column of chunk i
   template <typename F>
   __device__ __forceinline__ void each(int i, F f) const {
-    const int width = i < full ? L::V : rest;
-    const u4_vec w = i < full ? L::load(row + (uint32_t)i * L::V) : partial();
+    const bool whole = i < full;
+    const u4_vec w = whole ? L::load(body + (uint32_t)i * L::V) : partial();
 #pragma unroll
-    for (int c = 0; c < L::V; ++c)
-      if (c < width) f(i * L::V + c, L::at(w, c));
+    for (int c = 0; c < L::V; ++c) {
+      if (whole || c < rest) f(lead + i * L::V + c, L::at(w, c));
+      else if (DT != kF32 && c == L::V - 1 && lead != 0) f(0, L::at(w, c));
+    }
   }
 };
 
-// S, A and the maximum of the thread's chunks.  KEEP: the row is read again by this workgroup.
-template <int DT, int U, bool ENT, bool KEEP>
-__device__ __forceinline__ Stats thread_stats(const Segment<DT>& g, int T, float c) {
+// Loads batch b of the thread's whole chunks, U of them.  KEEP: the row is read again by this workgroup.
+template <int DT, int T, int U, bool KEEP>
+__device__ __forceinline__ void load_batch(const Segment<DT>& g, int b, u4_vec (&w)[U]) {
   using L = Logits<DT>;
-  Stats t = {kNegInf, 0.0f, 0.0f};
-  int i = threadIdx.x;
-  for (; i + (U - 1) * T < g.full; i += U * T) {
-    u4_vec w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const auto* p = g.row + (uint32_t)(i + u * T) * L::V;
-      w[u] = KEEP ? L::load(p) : L::load_once(p);
-    }
-    absorb<DT, U, ENT>(w, c, t);
+  for (int u = 0; u < U; ++u) {
+    const auto* p = g.body + (uint32_t)((int)threadIdx.x + (b * U + u) * T) * L::V;
+    w[u] = KEEP ? L::load(p) : L::load_once(p);
   }
-  if (i < g.full) {  // chunks past the last are -inf: they add nothing
-    u4_vec w[U];
+}
+
+// What the segment has beyond `batches` of U T whole chunks: fewer than U T, and the partial one.  The last chunk again where a thread has none, so that
+// all loads are made together; then the sums of what wavefronts have.  top: the loads' maxima, -inf past the end.
+template <int DT, int T, int U, bool ENT>
+__device__ __forceinline__ void absorb_rest(const Segment<DT>& g, int batches, float c, Running& t, u4_vec (&w)[U], u4_vec (&end)[1], float (&top)[U],
+                                            float (&end_top)[1]) {
+  using L = Logits<DT>;
+  const int i = threadIdx.x + batches * (U * T);
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = L::load(g.row + (uint32_t)min(i + u * T, g.full - 1) * L::V);
+  for (int u = 0; u < U; ++u)
+    if (g.full > 0) w[u] = L::load(g.body + (uint32_t)min(i + u * T, g.full - 1) * L::V);
+  end_top[0] = kNegInf;
+  end[0] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
+  const bool last = g.rest + g.lead != 0 && (int)threadIdx.x == g.full % T;
+  if (last) end[0] = g.partial();
 #pragma unroll
-    for (int u = 1; u < U; ++u)
+  for (int u = 0; u < U; ++u) {
+    top[u] = kNegInf;
+    if (i - (int)(threadIdx.x & 63) + u * T < g.full) {
       if (i + u * T >= g.full) w[u] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
-    absorb<DT, U, ENT>(w, c, t);
+      float m[1];
+      absorb<DT, 1, ENT, true>(reinterpret_cast<u4_vec(&)[1]>(w[u]), c, t, m);
+      top[u] = m[0];
+    }
   }
-  if (g.rest != 0 && (int)threadIdx.x == g.full % T) {
-    const u4_vec w[1] = {g.partial()};
-    absorb<DT, 1, ENT>(w, c, t);
+  if (last) absorb<DT, 1, ENT, true>(end, c, t, end_top);
+}
+
+// S, A and the maximum of the thread's chunks.
+template <int DT, int T, int U, bool ENT, bool KEEP>
+__device__ __forceinline__ Running thread_stats(const Segment<DT>& g, float c) {
+  Running t = {kNegInf, 0.0f, 0.0f};
+  u4_vec w[U], end[1];
+  float top[U], end_top[1];
+  const int batches = g.full / (U * T);
+  for (int b = 0; b < batches; ++b) {
+    load_batch<DT, T, U, KEEP>(g, b, w);
+    absorb<DT, U, ENT, false>(w, c, t, top);
   }
+  if (g.chunks() > batches * (U * T)) absorb_rest<DT, T, U, ENT>(g, batches, c, t, w, end, top, end_top);
   return t;
+}
+
+// A segment's sums about its maximum, in every thread, from each thread's.  `room` as for block_join.
+template <int DT, int W, bool ENT>
+__device__ __forceinline__ Stats segment_stats(const Segment<DT>& g, const Running& mine, float c, float4* room) {
+  const Running t = block_join<W, ENT>(mine, c, room);
+  if (fabsf(t.m * c) >= 1e37f && fabsf(t.m) < __builtin_inff()) {
+    // m c is no number to take differences from (a row of nothing but the type's lowest value, a very low temperature): x - m is
+    Stats u = {t.m, 0.0f, 0.0f};
+    for (int i = threadIdx.x; i < g.chunks(); i += 64 * W)
+      g.each(i, [&](int, float x) {
+        const float d = x - t.m, e = __builtin_amdgcn_exp2f(d * c);
+        u.s += e;
+        if (ENT) u.a = __builtin_fmaf(e, fmaxf(d, kFar), u.a);
+      });
+    u.s = wave_sum(u.s);
+    u.a = wave_sum(u.a);
+    if (W > 1) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = make_float4(u.m, u.s, u.a, 0.0f);
+      __syncthreads();
+      u.s = u.a = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        u.s += room[w].y;
+        u.a += room[w].z;
+      }
+    }
+    return u;
+  }
+  // from about r to about m: r's rounding goes out of the sums
+  const float off = t.m == kNegInf ? 0.0f : __builtin_fmaf(t.m, c, -reference(t.m, c)), f = __builtin_amdgcn_exp2f(-off);
+  return {t.m, t.s * f, ENT ? __builtin_fmaf(-off, t.s, t.a) * f / c : 0.0f};
 }
 
 // ---- top alternatives -----------------------------------------------------------------------------
 
-// The k largest of a row's columns, by value and then by column.  Every thread knows the largest logit it has seen; the k-th largest of
-// these is a floor under the k-th largest of the row, and only threads whose maximum reaches the floor can hold columns that do: about k
-// threads' columns are read again, and what reaches the floor, a little over k columns, is ranked by comparing each with each.
-// The floor is found as the top-k selections find theirs, by bisection on a threshold with early stopping: it need not be the k-th exactly.
-constexpr int kMaxCandidates = 1024;
-
-template <int T>
+// The k largest of a row's columns, by value and then by column, from the same pass.  The k-th largest of the threads' maxima is a floor under
+// the k-th largest of what they have seen; a column of the first batch, or of a later one, that reaches the floor is listed, and after 1, 2,
+// 4, 8 ... batches the floor is raised, so that each doubling lists about k columns.  Each wavefront has a list of its own, so that a place in it
+// is a count of lanes and no atomic, and drops what falls below a raised floor.  At the end what has reached the last floor, a little
+// over k columns, is ranked by comparing each with each.  The floor is found as the top-k selections find theirs, by
+// bisection on a threshold with early stopping: it need not be the k-th exactly.  (Reading the columns of the threads that reach the floor
+// again instead takes their lines from memory: 16 bytes used of 128, 8191 x 50000 fp32, k = 20, 397 us against 256.)
+template <int W>
 struct TopRoom {
-  uint64_t found[kMaxCandidates];
+  static constexpr int T = 64 * W;
+  static constexpr int kList = W == 1 ? 512 : (W == 4 ? 256 : 128);  // of a wavefront
+  static constexpr int kAll = W * kList;
+  uint64_t found[W][kList];
   uint64_t best[kMaxAlternatives];
   uint32_t key[T];
-  uint16_t holder[T];
+  int listed[W];
   uint32_t floor;
-  int holders, count;
+  int count, reach;
 };
 
-// A floor that at least k of the T keys reach, or 1 where fewer than k are not 0; the first wavefront's work.  Few more than k reach it
+template <bool MAX>
+__device__ __forceinline__ uint32_t wave_extreme(uint32_t v) {
+  const auto f = [](float a, float b) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    return __uint_as_float(MAX ? max(x, y) : min(x, y));
+  };
+  return __float_as_uint(wave_reduce(__uint_as_float(v), __uint_as_float(MAX ? 0u : 0xffffffffu), f));
+}
+
+// A floor that at least k of the T keys reach, or 0 where fewer than k are not 0; the first wavefront's work.  Few more than k reach it
 // unless many are equal.
 template <int T>
 __device__ __forceinline__ uint32_t find_floor(const uint32_t* keys, int k) {
@@ -263,16 +401,11 @@ __device__ __forceinline__ uint32_t find_floor(const uint32_t* keys, int k) {
     if (v[p] != 0) lo = min(lo, v[p]);
     hi = max(hi, v[p]);
   }
-  if (have <= k) return 1;
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
-  }
-  uint64_t a = __builtin_amdgcn_readfirstlane(lo), b = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(hi) + 1;
+  if (have < k) return 0;
+  uint32_t a = wave_extreme<false>(lo), b = wave_extreme<true>(hi) + 1;  // a is reached by k keys, b by fewer
   const int enough = k + max(8, k / 2);
-  while (b - a > 1) {  // a is reached by k keys, b by fewer
-    const uint32_t mid = (uint32_t)(a + (b - a) / 2);
+  while (b - a > 1) {
+    const uint32_t mid = a + (b - a) / 2;
     int n = 0;
 #pragma unroll
     for (int p = 0; p < P; ++p) n += __popcll(__ballot(v[p] >= mid));
@@ -283,18 +416,30 @@ __device__ __forceinline__ uint32_t find_floor(const uint32_t* keys, int k) {
       b = mid;
     }
   }
-  return (uint32_t)a;
+  return a;
 }
 
-// Ranks room.count (at most kMaxCandidates) distinct keys: the k largest in order in room.best, 0 where there are fewer.
-template <int T>
-__device__ __forceinline__ void rank_found(TopRoom<T>& room, int k) {
-  const int n = room.count;
-  for (int j = n + threadIdx.x; j < k; j += T) room.best[j] = 0;
-  for (int j = threadIdx.x; j < n; j += T) {
-    const uint64_t key = room.found[j];
+// The lists as one of n keys from the first on.
+template <int W>
+__device__ __forceinline__ void set_listed(TopRoom<W>& room, int n) {
+  if (threadIdx.x < W) room.listed[threadIdx.x] = min(max(n - (int)threadIdx.x * TopRoom<W>::kList, 0), TopRoom<W>::kList);
+}
+
+// Ranks the lists' distinct keys: the k largest in order in room.best, 0 where there are fewer.
+template <int W>
+__device__ __forceinline__ void rank_listed(TopRoom<W>& room, int k) {
+  const int wave = threadIdx.x >> 6, n = room.listed[wave];
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) all += room.listed[w];
+  for (int j = all + threadIdx.x; j < k; j += 64 * W) room.best[j] = 0;
+  for (int j = threadIdx.x & 63; j < n; j += 64) {
+    const uint64_t key = room.found[wave][j];
     int rank = 0;
-    for (int i = 0; i < n; ++i) rank += room.found[i] > key;
+    for (int w = 0; w < W; ++w) {
+      const int m = room.listed[w];
+      for (int i = 0; i < m; ++i) rank += room.found[w][i] > key;
+    }
     if (rank < k) room.best[rank] = key;
   }
   __syncthreads();
@@ -314,97 +459,202 @@ __device__ __forceinline__ int count_reaching(const Segment<DT>& g, uint32_t lea
   return n;
 }
 
-// The k largest of the segment in room.best, best first (0 where it has fewer columns); first: the segment's first column.
-// `mine`: the thread's maximum, or whatever (`any` false) where it has no column.
-template <int DT, int T>
-__device__ void segment_top(const Segment<DT>& g, int first, int k, float mine, bool any, TopRoom<T>& room) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t key = any ? order_key(mine) : 0;
-  room.key[threadIdx.x] = key;
-  if (threadIdx.x == 0) {
-    room.holders = 0;
-    room.count = 0;
+// Lists the columns of a load that reach the floor behind the wavefront's `n` (uniform); col(e): of the thread's element e.  n counts on past
+// the end.
+template <int DT, int W, typename F>
+__device__ __forceinline__ void list_chunk(const u4_vec& w, float floor, TopRoom<W>& room, int& n, F col) {
+  using L = Logits<DT>;
+  uint64_t* list = room.found[threadIdx.x >> 6];
+  u4_vec here = w;
+  asm volatile("" : "+v"(here));  // (else all loads are widened before the branch)
+#pragma unroll
+  for (int e = 0; e < L::V; ++e) {
+    const float v = L::at(here, e);
+    const uint64_t mask = __ballot(v >= floor);
+    if (mask != 0) {
+      const int at = (int)lanes_below(mask, (uint32_t)n);
+      if (v >= floor && at < TopRoom<W>::kList) list[at] = place_key(order_key(v), col(e));
+      n += __popcll(mask);
+    }
+  }
+}
+
+// Drops what lies below the floor from the wavefront's list.
+template <int W>
+__device__ __forceinline__ void drop_below(uint32_t least, TopRoom<W>& room, int& n) {
+  uint64_t* list = room.found[threadIdx.x >> 6];
+  const int lane = threadIdx.x & 63;
+  int kept = 0;
+  for (int i = 0; i < n; i += 64) {
+    const uint64_t key = i + lane < n ? list[i + lane] : 0;
+    const uint64_t mask = __ballot((uint32_t)(key >> 32) >= least);
+    if ((uint32_t)(key >> 32) >= least) list[lanes_below(mask, (uint32_t)kept)] = key;  // (at or before its place, after all lanes' reads)
+    kept += __popcll(mask);
+  }
+  n = kept;
+}
+
+// The floor under the k-th largest logit seen so far, in every thread: the smallest finite value where fewer than k threads have seen more
+// than -inf.
+template <int W>
+__device__ __forceinline__ float raise_floor(float seen, int k, TopRoom<W>& room) {
+  const uint32_t key = order_key(seen);
+  room.key[threadIdx.x] = key == kLowKey ? 0 : key;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const uint32_t f = find_floor<64 * W>(room.key, k);
+    if (threadIdx.x == 0) room.floor = f == 0 ? kLowKey + 1 : f;
   }
   __syncthreads();
-  if (wave == 0) {
-    const uint32_t f = find_floor<T>(room.key, k);
-    if (lane == 0) room.floor = f;
+  return order_value(room.floor);
+}
+
+// The first columns whose key is `least` follow the n of the first list up to k; the first wavefront's work.  Returns how many there are then.
+template <int DT, int W>
+__device__ int fill_list(const Segment<DT>& g, int first, int k, uint32_t least, int n, TopRoom<W>& room) {
+  uint64_t* list = room.found[0];
+  const int lane = threadIdx.x, chunks = g.chunks();
+  if (g.lead != 0 && n < k && order_key(Logits<DT>::widen(g.body[-1])) == least) {
+    if (lane == 0) list[n] = place_key(least, first);
+    ++n;
   }
+  for (int i = lane; n < k && i - lane < chunks; i += 64) {
+    int mine = 0;
+    if (i < chunks) g.each(i, [&](int col, float v) { mine += col >= g.lead && order_key(v) == least; });
+    int before = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(before, d);
+      if (lane >= d) before += o;
+    }
+    const int all = __shfl(before, 63);
+    before += n - mine;
+    if (mine > 0 && before < k)
+      g.each(i, [&](int col, float v) {
+        if (col >= g.lead && order_key(v) == least) {
+          if (before < k) list[before] = place_key(least, first + col);
+          ++before;
+        }
+      });
+    n += all;
+  }
+  return min(n, k);
+}
+
+// More columns reached the floors than there is room for: equal logits in crowds, or logits that ascend.  Bisection over the whole segment, until
+// so few columns reach the threshold that they can be listed, or none lies between the bounds; then the columns equal to it fill up.
+// `least` is reached by k columns.
+template <int DT, int W>
+__device__ void list_again(const Segment<DT>& g, int first, int k, uint32_t least, TopRoom<W>& room) {
+  constexpr int T = 64 * W, kAll = TopRoom<W>::kAll;
+  uint64_t a = least, b = (uint64_t)1 << 32;
+  int reach = g.lead + g.full * Logits<DT>::V + g.rest, above = 0;
+  bool next = true;  // the first threshold is the one above `least`: all others are equal where a mask has left few columns
+  while (b - a > 1 && reach > kAll) {
+    const uint32_t mid = next ? (uint32_t)(a + 1) : (uint32_t)(a + (b - a) / 2);
+    next = false;
+    const int n = count_reaching<DT, T>(g, mid, &room.reach);
+    if (n >= k) {
+      a = mid;
+      reach = n;
+    } else {
+      b = mid;
+      above = n;
+    }
+  }
+  const bool crowd = reach > kAll;  // fewer than k lie above `a`, too many equal it
+  const uint32_t listed = (uint32_t)a + (crowd ? 1 : 0);
+  if (threadIdx.x == 0) room.count = 0;
   __syncthreads();
-  uint32_t least = room.floor;
-  if (any && key >= least) room.holder[atomicAdd(&room.holders, 1)] = (uint16_t)threadIdx.x;
-  __syncthreads();
-  const int holders = room.holders, chunks = g.chunks();
-  for (int h = wave; h < holders; h += T / 64)
-    for (int64_t i = room.holder[h] + (int64_t)lane * T; i < chunks; i += 64 * T)
-      g.each((int)i, [&](int col, float v) {
+  if (!crowd || above > 0)
+    for (int i = threadIdx.x; i < g.chunks(); i += T)
+      g.each(i, [&](int col, float v) {
         const uint32_t o = order_key(v);
-        if (o >= least) {
+        if (o >= listed) {
           const int at = atomicAdd(&room.count, 1);
-          if (at < kMaxCandidates) room.found[at] = place_key(o, first + col);
+          if (at < kAll) room.found[0][at] = place_key(o, first + col);  // (the lists follow one another)
         }
       });
   __syncthreads();
-  if (room.count > kMaxCandidates) {
-    // Equal logits in crowds, or the largest ones in few threads' columns: bisection over the whole segment, until so few columns reach the
-    // threshold that they can be listed, or none lies between the bounds.  least is reached by k columns.
-    __syncthreads();  // (all have read the count)
-    uint64_t a = least, b = (uint64_t)1 << 32;
-    int reach = g.full * Logits<DT>::V + g.rest, above = 0;
-    bool next = true;  // the first threshold is the one above `least`: all others are equal where a mask has left few columns
-    while (b - a > 1 && reach > kMaxCandidates) {
-      const uint32_t mid = next ? (uint32_t)(a + 1) : (uint32_t)(a + (b - a) / 2);
-      next = false;
-      const int n = count_reaching<DT, T>(g, mid, &room.holders);
-      if (n >= k) {
-        a = mid;
-        reach = n;
-      } else {
-        b = mid;
-        above = n;
-      }
+  int n = room.count;
+  __syncthreads();
+  if (crowd) {
+    if (threadIdx.x < 64) {
+      n = fill_list<DT, W>(g, first, k, (uint32_t)a, n, room);
+      if (threadIdx.x == 0) room.count = n;
     }
-    least = (uint32_t)a;
-    const uint32_t listed = reach > kMaxCandidates ? least + 1 : least;  // (least is then below the largest key of all)
-    if (threadIdx.x == 0) room.count = 0;
     __syncthreads();
-    if (reach <= kMaxCandidates || above > 0)
-      for (int i = threadIdx.x; i < chunks; i += T)
-        g.each(i, [&](int col, float v) {
-          const uint32_t o = order_key(v);
-          if (o >= listed) {
-            const int at = atomicAdd(&room.count, 1);
-            if (at < kMaxCandidates) room.found[at] = place_key(o, first + col);
-          }
-        });
-    __syncthreads();
-    if (reach > kMaxCandidates && wave == 0) {  // fewer than k lie above `least`: the first columns that equal it fill up
-      int n = room.count;
-      for (int i = lane; n < k && i - lane < chunks; i += 64) {
-        int mine_n = 0;
-        if (i < chunks) g.each(i, [&](int, float v) { mine_n += order_key(v) == least; });
-        int before = mine_n;
+    n = room.count;
+  }
+  set_listed(room, n);
+  __syncthreads();
+}
+
+// thread_stats, and the k largest of the segment in room.best, best first (0 where it has fewer columns); first: the segment's first column.
+template <int DT, int W, int U, bool ENT>
+__device__ Running stats_and_top(const Segment<DT>& g, int first, int k, float c, TopRoom<W>& room) {
+  using L = Logits<DT>;
+  constexpr int T = 64 * W, kList = TopRoom<W>::kList;
+  Running t = {kNegInf, 0.0f, 0.0f};
+  float floor = 0.0f;
+  int n = 0;  // the wavefront's list
+  bool lost = false;
+  const auto raise = [&] {
+    floor = raise_floor<W>(t.m, k, room);
+    lost |= n > kList;
+    drop_below<W>(order_key(floor), room, n);
+  };
+  const auto list = [&](const u4_vec(&w)[U], const float(&top)[U], int b) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int o = __shfl_up(before, d);
-          if (lane >= d) before += o;
-        }
-        const int all = __shfl(before, 63);
-        before += n - mine_n;
-        if (mine_n > 0 && before < k)
-          g.each(i, [&](int col, float v) {
-            if (order_key(v) == least) {
-              if (before < k) room.found[before] = place_key(least, first + col);
-              ++before;
-            }
-          });
-        n += all;
+    for (int u = 0; u < U; ++u)
+      if (__any(top[u] >= floor)) {
+        const int col = first + g.lead + ((int)threadIdx.x + (b * U + u) * T) * L::V;
+        list_chunk<DT, W>(w[u], floor, room, n, [&](int e) { return col + e; });
       }
-      if (lane == 0) room.count = min(n, k);
+  };
+  u4_vec w[U];
+  float top[U];
+  const int batches = g.full / (U * T);
+  for (int b = 0; b < batches; ++b) {
+    load_batch<DT, T, U, false>(g, b, w);
+    absorb<DT, U, ENT, false>(w, c, t, top);
+    if ((b & (b + 1)) == 0) raise();
+    list(w, top, b);
+  }
+  if (g.chunks() > batches * (U * T)) {
+    u4_vec end[1];
+    float end_top[1];
+    absorb_rest<DT, T, U, ENT>(g, batches, c, t, w, end, top, end_top);
+    raise();
+    list(w, top, batches);
+    if (__any(end_top[0] >= floor))
+      list_chunk<DT, W>(end[0], floor, room, n, [&](int e) { return e < g.rest ? first + g.lead + g.full * L::V + e : first; });
+  } else if ((batches & (batches - 1)) != 0) {
+    raise();
+  }
+  lost |= n > kList;
+  if ((threadIdx.x & 63) == 0) room.listed[threadIdx.x >> 6] = lost ? kList + 1 : n;
+  __syncthreads();
+  int all = 0;
+  bool again = false;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    all += room.listed[w];
+    again |= room.listed[w] > kList;
+  }
+  if (again) {
+    __syncthreads();
+    list_again<DT, W>(g, first, k, order_key(floor), room);
+  } else if (all < k) {  // all finite ones are listed: those that are not follow in the first list
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const int filled = fill_list<DT, W>(g, first, k - all + n, kLowKey, n, room);
+      if (threadIdx.x == 0) room.listed[0] = filled;
     }
     __syncthreads();
   }
-  rank_found<T>(room, k);
+  rank_listed<W>(room, k);
+  return t;
 }
 
 // ---- given tokens and the teacher's entries -------------------------------------------------------
@@ -431,7 +681,7 @@ struct ListRoom {
 // The first wavefront writes the row's list to LDS; entries that do not count have column -1 and weight 0.
 __device__ __forceinline__ void teacher_list(const LogitsArgs& a, int64_t n, ListRoom& r) {
   const int lane = threadIdx.x;
-  const float c = a.inv_t * kLog2e;
+  const float c = a.c;
   float top = kNegInf;
   bool ascending = true;
   for (int j = lane; j < a.k; j += 64) {
@@ -518,9 +768,9 @@ __device__ __forceinline__ void write_tokens(const LogitsArgs& a, int64_t n, con
   }
 }
 
-template <int T>
-__device__ __forceinline__ void write_top(const LogitsArgs& a, int64_t n, const Stats& t, float ln_s, const TopRoom<T>& room) {
-  for (int j = threadIdx.x; j < a.k; j += T) {
+template <int W>
+__device__ __forceinline__ void write_top(const LogitsArgs& a, int64_t n, const Stats& t, float ln_s, const TopRoom<W>& room) {
+  for (int j = threadIdx.x; j < a.k; j += 64 * W) {
     const uint64_t key = room.best[j];
     a.top_logprobs[n * a.k + j] = t.s == 0.0f ? kNegInf : (order_value((uint32_t)(key >> 32)) - t.m) * a.inv_t - ln_s;
     a.top_cols[n * a.k + j] = place_col(key);
@@ -540,21 +790,22 @@ __global__ __launch_bounds__(64 * W) void logits_rows_kernel(LogitsArgs a) {
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
   const int first = seg * a.seg_cols;
   const Segment<DT> g(row + first, min(a.seg_cols, a.M - first));
-  const float c = a.inv_t * kLog2e;
+  const float c = a.c;
   __shared__ typename std::conditional<OP == kOpDistill && !SPLIT, ListRoom, int>::type list;
   if constexpr (OP == kOpDistill && !SPLIT) {
     if (threadIdx.x < 64) teacher_list(a, n, list);
   }
-  const Stats mine = thread_stats<DT, 4, ENT, TOP>(g, T, c);
-  const Stats t = block_join<W, ENT>(mine, c, sums);
-  if constexpr (TOP) {
-    __shared__ TopRoom<T> room;
-    segment_top<DT, T>(g, first, a.k, mine.m, (int)threadIdx.x < g.chunks(), room);
+  Stats t;
+  if constexpr (!TOP) {
+    t = segment_stats<DT, W, ENT>(g, thread_stats<DT, T, 4, ENT, false>(g, c), c, sums);
+  } else {
+    __shared__ TopRoom<W> room;
+    t = segment_stats<DT, W, ENT>(g, stats_and_top<DT, W, 4, ENT>(g, first, a.k, c, room), c, sums);
     if constexpr (SPLIT) {
       uint64_t* keys = a.part_keys + (n * a.segments + seg) * a.k;
       for (int j = threadIdx.x; j < a.k; j += T) keys[j] = room.best[j];
     } else {
-      write_top<T>(a, n, t, logf(t.s), room);
+      write_top<W>(a, n, t, logf(t.s), room);
     }
   }
   if constexpr (SPLIT) {
@@ -570,11 +821,11 @@ __global__ __launch_bounds__(64 * W) void logits_rows_kernel(LogitsArgs a) {
   }
 }
 
-// Sums of a row's segments, in every thread of a workgroup of W wavefronts.
-template <int W, bool ENT>
-__device__ __forceinline__ Stats join_segments(const LogitsArgs& a, int64_t n, float c, float4* room) {
+// Sums of a row's segments, in every lane: each wavefront takes them all.
+template <bool ENT>
+__device__ __forceinline__ Stats join_segments(const LogitsArgs& a, int64_t n, float c) {
   Stats t = {kNegInf, 0.0f, 0.0f};
-  for (int s = threadIdx.x; s < a.segments; s += 64 * W) {
+  for (int s = threadIdx.x & 63; s < a.segments; s += 64) {
     const float4 p = a.part[n * a.segments + s];
     Stats u = {p.x, p.y, p.z};
     const float m = fmaxf(t.m, u.m);
@@ -583,25 +834,27 @@ __device__ __forceinline__ Stats join_segments(const LogitsArgs& a, int64_t n, f
     t.s += u.s;
     t.a += u.a;
   }
-  return block_join<W, ENT>(t, c, room);
+  scale_to<ENT>(t, wave_max(t.m), c);
+  t.s = wave_sum(t.s);
+  if (ENT) t.a = wave_sum(t.a);
+  return t;
 }
 
 template <int DT, int OP, bool TOP>
 __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
   using L = Logits<DT>;
   constexpr int T = 256;
-  __shared__ float4 sums[4];
   const int64_t n = a.row0 + blockIdx.x;
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
   __shared__ typename std::conditional<OP == kOpDistill, ListRoom, int>::type list;
   if constexpr (OP == kOpDistill) {
     if (threadIdx.x < 64) teacher_list(a, n, list);
   }
-  const Stats t = join_segments<4, OP == kOpTokens>(a, n, a.inv_t * kLog2e, sums);
+  const Stats t = join_segments<OP == kOpTokens>(a, n, a.c);
   const float ln_s = logf(t.s);
   if constexpr (TOP) {
     // the segments' alternatives, merged as a segment's columns are: each thread's largest, a floor, what reaches it
-    __shared__ TopRoom<T> room;
+    __shared__ TopRoom<4> room;
     const uint64_t* keys = a.part_keys + n * a.segments * a.k;
     const int all = a.segments * a.k;  // at most kMaxMergeKeys
     constexpr int P = kMaxMergeKeys / T;
@@ -621,7 +874,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
       if (threadIdx.x == 0) room.floor = f;
     }
     __syncthreads();
-    uint64_t least = (uint64_t)room.floor << 32;
+    uint64_t least = (uint64_t)max(room.floor, 1u) << 32;  // (0: all that are keys)
     int n_reach = 0;
 #pragma unroll
     for (int p = 0; p < P; ++p) n_reach += v[p] >= least;
@@ -631,7 +884,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
     __syncthreads();
     // more than there is room for: bisection on the whole keys, which are distinct
     uint64_t b = ~(uint64_t)0;
-    while (reach > kMaxCandidates) {
+    while (reach > TopRoom<4>::kAll) {
       const uint64_t mid = least + (b - least) / 2;
       if (threadIdx.x == 0) room.count = 0;
       __syncthreads();
@@ -653,10 +906,12 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if (v[p] >= least) room.found[atomicAdd(&room.count, 1)] = v[p];
+      if (v[p] >= least) room.found[0][atomicAdd(&room.count, 1)] = v[p];
     __syncthreads();
-    rank_found<T>(room, a.k);
-    write_top<T>(a, n, t, ln_s, room);
+    set_listed(room, room.count);
+    __syncthreads();
+    rank_listed<4>(room, a.k);
+    write_top<4>(a, n, t, ln_s, room);
   }
   if constexpr (OP == kOpTokens) {
     write_tokens<DT>(a, n, row, t, ln_s, T);
@@ -697,17 +952,18 @@ __device__ __forceinline__ void write_base(const Segment<DT>& g, typename Logits
     for (int c = 0; c < L::V; ++c) y[c] = base.template at<ENT>(L::at(w, c));
     return L::pack(y);
   };
+  typename L::elem* to = out + g.lead;
   for (; i + (U - 1) * T < g.full; i += U * T) {
     u4_vec w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = ZERO ? none : L::load_once(g.row + (uint32_t)(i + u * T) * L::V);
+    for (int u = 0; u < U; ++u) w[u] = ZERO ? none : L::load_once(g.body + (uint32_t)(i + u * T) * L::V);
 #pragma unroll
-    for (int u = 0; u < U; ++u) L::store(out + (uint32_t)(i + u * T) * L::V, ZERO ? none : turn(w[u]));
+    for (int u = 0; u < U; ++u) L::store(to + (uint32_t)(i + u * T) * L::V, ZERO ? none : turn(w[u]));
   }
-  for (; i < g.full; i += T) L::store(out + (uint32_t)i * L::V, ZERO ? none : turn(L::load_once(g.row + (uint32_t)i * L::V)));
-  if ((int)threadIdx.x < g.rest) {
-    const uint32_t at = (uint32_t)g.full * L::V + threadIdx.x;
-    out[at] = ZERO ? L::narrow(0.0f) : L::narrow(base.template at<ENT>(L::widen(g.row[at])));
+  for (; i < g.full; i += T) L::store(to + (uint32_t)i * L::V, ZERO ? none : turn(L::load_once(g.body + (uint32_t)i * L::V)));
+  if ((int)threadIdx.x < g.rest + g.lead) {
+    const int64_t at = (int)threadIdx.x < g.rest ? (int64_t)g.full * L::V + threadIdx.x : -1;
+    to[at] = ZERO ? L::narrow(0.0f) : L::narrow(base.template at<ENT>(L::widen(g.body[at])));
   }
 }
 
@@ -762,7 +1018,7 @@ __device__ __forceinline__ void write_gradient(const LogitsArgs& a, const ListRo
     return;
   }
   float x[(kMaxList + T - 1) / T];
-  read_list<DT, T>(a, r, first, cols, g.row, x);
+  read_list<DT, T>(a, r, first, cols, g.body - g.lead, x);
   __syncthreads();
   write_base<DT, 4, ENT, false>(g, out, T, base);
   __syncthreads();
@@ -791,7 +1047,8 @@ __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
   base.inv_t = a.inv_t;
   bool empty;
   if constexpr (JOIN) {
-    const Stats t = join_segments<4, false>(a, n, a.inv_t * kLog2e, sums);
+    __syncthreads();
+    const Stats t = join_segments<false>(a, n, a.c);
     base.m = t.m;
     base.less = logf(t.s);
     empty = t.s == 0.0f;
@@ -805,7 +1062,8 @@ __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
     empty = base.less == kNegInf;
     __syncthreads();
     if (fabsf(base.less) > kLargeLse && fabsf(base.less) < __builtin_inff()) {
-      const Stats t = block_join<4, false>(thread_stats<DT, 4, false, true>(Segment<DT>(row, a.M), T, a.inv_t * kLog2e), a.inv_t * kLog2e, sums);
+      const Segment<DT> all(row, a.M);
+      const Stats t = segment_stats<DT, 4, false>(all, thread_stats<DT, T, 4, false, true>(all, a.c), a.c, sums);
       base.m = t.m;
       base.less = logf(t.s);
     }
@@ -837,7 +1095,7 @@ __global__ __launch_bounds__(64 * W) void distill_row_kernel(LogitsArgs a) {
     write_base<DT, 4, false, true>(g, out, T, base);
     return;
   }
-  const Stats t = block_join<W, false>(thread_stats<DT, 4, false, true>(g, T, a.inv_t * kLog2e), a.inv_t * kLog2e, sums);
+  const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, 4, false, true>(g, a.c), a.c, sums);
   base.m = t.m;
   base.less = logf(t.s);
   if (threadIdx.x < 64) {

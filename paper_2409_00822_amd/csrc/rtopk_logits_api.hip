@@ -41,13 +41,15 @@ int rows_of_logits(LogitsArgs& a, const void* logits, int32_t dtype, int64_t N, 
   if (N < 0 || M < 1 || (N > 1 && stride < M)) return RTOPK_ERR_BAD_SHAPE;
   if (M > rtopk::kMaxLogitsM) return RTOPK_ERR_M_TOO_LARGE;
   const float inv_t = 1.0f / temperature;
-  if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(inv_t) || !(inv_t > 0.0f)) return RTOPK_ERR_BAD_TEMPERATURE;
+  const float c = (float)(1.44269504088896340736 / (double)temperature);
+  if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(c)) return RTOPK_ERR_BAD_TEMPERATURE;
   if (N > 0 && stride > (INT64_MAX / 8) / N) return RTOPK_ERR_BAD_SHAPE;
   a.x = logits;
   a.N = N;
   a.M = M;
   a.stride = stride;
   a.inv_t = inv_t;
+  a.c = c;
   return RTOPK_OK;
 }
 

@@ -19,7 +19,7 @@ struct LogitsArgs {
   int64_t N, stride;
   int64_t row0;   // first row of the launch
   int M, k;       // k: alternatives (forward, tokens), given tokens (backward, tokens) or the teacher's entries
-  float inv_t;    // 1 / temperature
+  float inv_t, c; // 1 / temperature, log2(e) / temperature
   const void* tokens;  // [N][tokens_per_row], 32 or 64 bits
   int tokens_per_row, token64;
   const void* teacher_vals;  // [N][k]
