@@ -9,10 +9,11 @@ template <int DT, int OP, bool TOP>
 hipError_t rows_of(int waves, bool split, const LogitsArgs& a, int64_t rows, hipStream_t s) {
   if (split) return launch_kernel(logits_rows_kernel<DT, 4, OP, TOP, true>, dim3((uint32_t)(rows * a.segments)), dim3(256), 0, s, a);
   const dim3 grid((uint32_t)rows);
+  const size_t lds = OP == kOpDistill ? list_bytes(a.k) : 0;
   switch (waves) {
-    case 1: return launch_kernel(logits_rows_kernel<DT, 1, OP, TOP, false>, grid, dim3(64), 0, s, a);
-    case 4: return launch_kernel(logits_rows_kernel<DT, 4, OP, TOP, false>, grid, dim3(256), 0, s, a);
-    default: return launch_kernel(logits_rows_kernel<DT, 16, OP, TOP, false>, grid, dim3(1024), 0, s, a);
+    case 1: return launch_kernel(logits_rows_kernel<DT, 1, OP, TOP, false>, grid, dim3(64), lds, s, a);
+    case 4: return launch_kernel(logits_rows_kernel<DT, 4, OP, TOP, false>, grid, dim3(256), lds, s, a);
+    default: return launch_kernel(logits_rows_kernel<DT, 16, OP, TOP, false>, grid, dim3(1024), lds, s, a);
   }
 }
 
@@ -25,7 +26,7 @@ hipError_t rows_of_type(int op, int waves, bool split, const LogitsArgs& a, int6
 template <int DT>
 hipError_t join_of_type(int op, const LogitsArgs& a, int64_t rows, hipStream_t s) {
   const dim3 grid((uint32_t)rows), block(256);
-  if (op == kOpDistill) return launch_kernel(logits_join_kernel<DT, kOpDistill, false>, grid, block, 0, s, a);
+  if (op == kOpDistill) return launch_kernel(logits_join_kernel<DT, kOpDistill, false>, grid, block, list_bytes(a.k), s, a);
   return a.k > 0 ? launch_kernel(logits_join_kernel<DT, kOpTokens, true>, grid, block, 0, s, a)
                  : launch_kernel(logits_join_kernel<DT, kOpTokens, false>, grid, block, 0, s, a);
 }

@@ -9,20 +9,20 @@ template <int DT>
 hipError_t grad_of_type(int op, bool join, const LogitsArgs& a, int64_t rows, hipStream_t s) {
   const dim3 grid((uint32_t)(rows * a.segments)), block(256);
   if (op == kOpDistill)
-    return join ? launch_kernel(logits_grad_kernel<DT, kOpDistill, false, true>, grid, block, 0, s, a)
-                : launch_kernel(logits_grad_kernel<DT, kOpDistill, false, false>, grid, block, 0, s, a);
-  return a.grad_entropy ? launch_kernel(logits_grad_kernel<DT, kOpTokens, true, false>, grid, block, 0, s, a)
-                        : launch_kernel(logits_grad_kernel<DT, kOpTokens, false, false>, grid, block, 0, s, a);
+    return join ? launch_kernel(logits_grad_kernel<DT, kOpDistill, false, true>, grid, block, list_bytes(a.k), s, a)
+                : launch_kernel(logits_grad_kernel<DT, kOpDistill, false, false>, grid, block, list_bytes(a.k), s, a);
+  return a.grad_entropy ? launch_kernel(logits_grad_kernel<DT, kOpTokens, true, false>, grid, block, list_bytes(a.k), s, a)
+                        : launch_kernel(logits_grad_kernel<DT, kOpTokens, false, false>, grid, block, list_bytes(a.k), s, a);
 }
 
 template <int DT>
-hipError_t row_of_type(int waves, const LogitsArgs& a, int64_t rows, hipStream_t s) {
-  const dim3 grid((uint32_t)rows);
-  switch (waves) {
-    case 1: return launch_kernel(distill_row_kernel<DT, 1>, grid, dim3(64), 0, s, a);
-    case 4: return launch_kernel(distill_row_kernel<DT, 4>, grid, dim3(256), 0, s, a);
-    default: return launch_kernel(distill_row_kernel<DT, 16>, grid, dim3(1024), 0, s, a);
-  }
+hipError_t row_of_type(int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t s) {
+  const dim3 grid((uint32_t)rows), block((uint32_t)(64 * waves));
+#define X(w, r, q) \
+  if (waves == w && loads == r + q) return launch_kernel(distill_held_kernel<DT, w, r, q>, grid, block, list_bytes(a.k), s, a);
+  RTOPK_HELD_LIST(X)
+#undef X
+  return launch_kernel(distill_row_kernel<DT, 8>, grid, dim3(512), list_bytes(a.k), s, a);
 }
 
 }  // namespace
@@ -33,8 +33,8 @@ hipError_t launch_logits_grad(int dtype, int op, bool join, const LogitsArgs& a,
                          : grad_of_type<kBF16>(op, join, a, rows, s);
 }
 
-hipError_t launch_distill_row(int dtype, int waves, const LogitsArgs& a, int64_t rows, hipStream_t s) {
-  return dtype == kF32 ? row_of_type<kF32>(waves, a, rows, s) : dtype == kF16 ? row_of_type<kF16>(waves, a, rows, s) : row_of_type<kBF16>(waves, a, rows, s);
+hipError_t launch_distill_row(int dtype, int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t s) {
+  return dtype == kF32 ? row_of_type<kF32>(waves, loads, a, rows, s) : dtype == kF16 ? row_of_type<kF16>(waves, loads, a, rows, s) : row_of_type<kBF16>(waves, loads, a, rows, s);
 }
 
 }  // namespace rtopk

@@ -157,6 +157,9 @@ __device__ __forceinline__ void rise_to(Running& t, float m, float c) {
   t.m = m;
 }
 
+// Whether differences from m c say nothing.
+__device__ __forceinline__ bool far_maximum(float m, float c) { return fabsf(m * c) >= 1e37f && fabsf(m) < __builtin_inff(); }
+
 // All W wavefronts' sums, in every thread.  `room`: W entries; a barrier lies between its writes and reads.
 template <int W, bool ENT>
 __device__ __forceinline__ Running block_join(Running t, float c, float4* room) {
@@ -326,7 +329,7 @@ __device__ __forceinline__ Running thread_stats(const Segment<DT>& g, float c) {
 template <int DT, int W, bool ENT>
 __device__ __forceinline__ Stats segment_stats(const Segment<DT>& g, const Running& mine, float c, float4* room) {
   const Running t = block_join<W, ENT>(mine, c, room);
-  if (fabsf(t.m * c) >= 1e37f && fabsf(t.m) < __builtin_inff()) {
+  if (far_maximum(t.m, c)) {
     // m c is no number to take differences from (a row of nothing but the type's lowest value, a very low temperature): x - m is
     Stats u = {t.m, 0.0f, 0.0f};
     for (int i = threadIdx.x; i < g.chunks(); i += 64 * W)
@@ -670,13 +673,29 @@ __device__ __forceinline__ float teacher_at(const LogitsArgs& a, int64_t i) {
   return a.teacher_dtype == kBF16 ? Logits<kBF16>::widen(h) : Logits<kF16>::widen(h);
 }
 
-struct ListRoom {
-  int col[kMaxList];
-  float w[kMaxList];   // the teacher's probability, or the gradient that belongs to a token
-  float lp[kMaxList];  // logarithm of the former
-  float mass;          // sum of w
-  int ascending;       // columns in strictly ascending order, so none twice
+// Whether the row has an entry that counts, looked up by each wavefront for itself.
+__device__ __forceinline__ bool any_entry(const LogitsArgs& a, int64_t n) {
+  for (int j = threadIdx.x & 63; j - (int)(threadIdx.x & 63) < a.k; j += 64) {
+    const int col = j < a.k ? a.teacher_cols[n * a.k + j] : -1;
+    if (__any(col >= 0 && col < a.M && teacher_at(a, n * a.k + j) > kNegInf)) return true;
+  }
+  return false;
+}
+
+// A row's list in LDS: three values to an entry in the launch's dynamic memory (list_bytes), so that short lists leave room for more workgroups.
+struct ListHead {
+  float mass;     // sum of w
+  int ascending;  // columns in strictly ascending order, so none twice
 };
+struct ListRoom {
+  int* col;
+  float* w;   // the teacher's probability, or the gradient that belongs to a token
+  float* lp;  // logarithm of the former
+  ListHead& head;
+  __device__ __forceinline__ ListRoom(float* memory, int k, ListHead& h)
+      : col(reinterpret_cast<int*>(memory)), w(memory + k), lp(memory + 2 * k), head(h) {}
+};
+inline size_t list_bytes(int k) { return 12 * (size_t)k; }
 
 // The first wavefront writes the row's list to LDS; entries that do not count have column -1 and weight 0.
 __device__ __forceinline__ void teacher_list(const LogitsArgs& a, int64_t n, ListRoom& r) {
@@ -716,8 +735,8 @@ __device__ __forceinline__ void teacher_list(const LogitsArgs& a, int64_t n, Lis
   mass = wave_sum(mass);
   const bool all = __all(ascending);
   if (lane == 0) {
-    r.mass = mass;
-    r.ascending = all;
+    r.head.mass = mass;
+    r.head.ascending = all;
   }
 }
 
@@ -733,8 +752,8 @@ __device__ __forceinline__ void token_list(const LogitsArgs& a, int64_t n, ListR
   }
   mass = wave_sum(mass);
   if (lane == 0) {
-    r.mass = mass;
-    r.ascending = a.k == 1;
+    r.head.mass = mass;
+    r.head.ascending = a.k == 1;
   }
 }
 
@@ -791,7 +810,9 @@ __global__ __launch_bounds__(64 * W) void logits_rows_kernel(LogitsArgs a) {
   const int first = seg * a.seg_cols;
   const Segment<DT> g(row + first, min(a.seg_cols, a.M - first));
   const float c = a.c;
-  __shared__ typename std::conditional<OP == kOpDistill && !SPLIT, ListRoom, int>::type list;
+  extern __shared__ float list_memory[];
+  __shared__ ListHead head;
+  ListRoom list(list_memory, a.k, head);  // (distillation only)
   if constexpr (OP == kOpDistill && !SPLIT) {
     if (threadIdx.x < 64) teacher_list(a, n, list);
   }
@@ -846,7 +867,9 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
   constexpr int T = 256;
   const int64_t n = a.row0 + blockIdx.x;
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
-  __shared__ typename std::conditional<OP == kOpDistill, ListRoom, int>::type list;
+  extern __shared__ float list_memory[];
+  __shared__ ListHead head;
+  ListRoom list(list_memory, a.k, head);  // (distillation only)
   if constexpr (OP == kOpDistill) {
     if (threadIdx.x < 64) teacher_list(a, n, list);
   }
@@ -967,9 +990,24 @@ __device__ __forceinline__ void write_base(const Segment<DT>& g, typename Logits
   }
 }
 
-// The columns of the list that lie in the segment, after the base has been written (a barrier lies between): one value, rounded once, from
-// the thread of the column's first entry.  `x`: the logits at the thread's entries, read before the base was written (the gradient may lie
-// in the logits' place).  sign * r.w: what an entry adds.
+// Entry j of the list, after the base has been written (a barrier lies between): where its column lies in the segment and no earlier entry has
+// it, the column's one value, rounded once.  base_y: the base at the column; factor * weight(i): what an entry adds.
+template <int DT, typename F>
+__device__ __forceinline__ void write_entry(const LogitsArgs& a, const ListRoom& r, int j, int first, int cols, typename Logits<DT>::elem* out,
+                                            float factor, float base_y, F weight) {
+  const int col = r.col[j];
+  if (col < first || col >= first + cols) return;
+  float w = weight(j);
+  if (!r.head.ascending)
+    for (int i = 0; i < a.k; ++i)
+      if (i != j && r.col[i] == col) {
+        if (i < j) return;
+        w += weight(i);
+      }
+  out[col - first] = Logits<DT>::narrow(__builtin_fmaf(factor, w, base_y));
+}
+
+// All entries.  `x`: the logits at the thread's entries, read before the base was written (the gradient may lie in the logits' place).
 template <int DT, int T, bool ENT, bool ZERO>
 __device__ __forceinline__ void write_list(const LogitsArgs& a, const ListRoom& r, int first, int cols, typename Logits<DT>::elem* out,
                                            const Base& base, float factor, const float (&x)[(kMaxList + T - 1) / T]) {
@@ -977,19 +1015,7 @@ __device__ __forceinline__ void write_list(const LogitsArgs& a, const ListRoom& 
   for (int e = 0; e < (kMaxList + T - 1) / T; ++e) {
     const int j = threadIdx.x + e * T;
     if (j >= a.k) break;
-    const int col = r.col[j];
-    if (col < first || col >= first + cols) continue;
-    float w = r.w[j];
-    bool again = false;
-    if (!r.ascending)
-      for (int i = 0; i < a.k; ++i)
-        if (i != j && r.col[i] == col) {
-          if (i < j) again = true;
-          w += r.w[i];
-        }
-    if (again) continue;
-    const float y = ZERO ? 0.0f : base.template at<ENT>(x[e]);
-    out[col - first] = Logits<DT>::narrow(__builtin_fmaf(factor, w, y));
+    write_entry<DT>(a, r, j, first, cols, out, factor, ZERO ? 0.0f : base.template at<ENT>(x[e]), [&](int i) { return r.w[i]; });
   }
 }
 
@@ -1031,7 +1057,9 @@ template <int DT, int OP, bool ENT, bool JOIN>
 __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
   using L = Logits<DT>;
   constexpr int T = 256;
-  __shared__ ListRoom list;
+  extern __shared__ float list_memory[];
+  __shared__ ListHead head;
+  ListRoom list(list_memory, a.k, head);
   __shared__ float4 sums[4];
   const int seg = (int)(blockIdx.x % (uint32_t)a.segments);
   const int64_t n = a.row0 + blockIdx.x / (uint32_t)a.segments;
@@ -1069,19 +1097,144 @@ __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
     }
   }
   const float up = OP == kOpTokens ? a.inv_t : a.inv_t * a.grad[n];
-  base.alpha = OP == kOpTokens ? -up * list.mass : up * list.mass;
+  base.alpha = OP == kOpTokens ? -up * head.mass : up * head.mass;
   base.beta = ENT ? a.inv_t * a.grad_entropy[n] : 0.0f;
   base.h = ENT ? a.entropy_in[n] : 0.0f;
   const bool zero = empty || (base.alpha == 0.0f && base.beta == 0.0f);
   write_gradient<DT, T, ENT>(a, list, g, first, cols, out + first, base, empty ? 0.0f : (OP == kOpTokens ? up : -up), zero);
 }
 
-// Loss and gradient of a row by one workgroup: the row is read twice, the second time from the caches.
+// Loss and gradient of a row by one workgroup that holds it on chip, so that it is read once and its gradient written once: R loads of each thread in
+// registers and, for the widest rows, Q more in LDS.  The first Q loads go on to LDS once they are in the sums, and their registers take
+// the last Q.  With eight wavefronts and 128 registers each, two such workgroups share a compute unit, and one's loads and stores overlap
+// the other's arithmetic.
+template <int DT, int W, int R, int Q>
+__global__ __launch_bounds__(64 * W, R + Q > 16 && W == 8 ? 4 : 1) void distill_held_kernel(LogitsArgs a) {
+  using L = Logits<DT>;
+  constexpr int T = 64 * W;
+  constexpr int G = R > 16 ? 2 : 4;  // loads that are summed together: more take registers that the row needs
+  static_assert(R % G == 0 && Q % G == 0 && Q <= R, "whole groups");
+  extern __shared__ float list_memory[];
+  __shared__ ListHead head;
+  ListRoom list(list_memory, a.k, head);  // (w: the logits at the list's columns)
+  __shared__ float4 sums[W];
+  __shared__ u4_vec room[Q > 0 ? Q : 1][Q > 0 ? T : 1];
+  const int64_t n = a.row0 + blockIdx.x;
+  const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
+  auto* out = static_cast<typename L::elem*>(a.grad_x) + n * a.grad_stride;
+  const Segment<DT> g(row, a.M);
+  Base base = {0.0f, 0.0f, 0.0f, 0.0f, a.inv_t, 0.0f};
+  if (!any_entry(a, n)) {  // no loss, and a gradient of zero whatever the logits are
+    if (threadIdx.x == 0) a.loss[n] = 0.0f;
+    write_base<DT, 4, false, true>(g, out, T, base);
+    return;
+  }
+  const int wave0 = (int)threadIdx.x - (int)(threadIdx.x & 63);  // what a wavefront has of a load is decided for all its lanes
+  const auto load = [&](int chunk, u4_vec& w) {  // chunk: without the thread's own number
+    if (wave0 + chunk < g.full) w = L::load_once(g.body + (uint32_t)min((int)threadIdx.x + chunk, g.full - 1) * L::V);
+  };
+  u4_vec w[R], end[1];
+#pragma unroll
+  for (int u = 0; u < R; ++u) load(u * T, w[u]);
+  const bool last = g.rest + g.lead != 0 && (int)threadIdx.x == g.full % T;
+  if (last) end[0] = g.partial();
+  if (threadIdx.x < 64) {
+    teacher_list(a, n, list);
+    for (int j = threadIdx.x; j < a.k; j += 64) list.w[j] = list.col[j] >= 0 ? L::widen(row[list.col[j]]) : 0.0f;
+  }
+  Running mine = {kNegInf, 0.0f, 0.0f};
+  const auto sum = [&](u4_vec(&four)[G], int u) {  // loads u ... u + G - 1
+    float top[G], one[1];
+    if (wave0 + 63 + (u + G - 1) * T < g.full) {
+      absorb<DT, G, false, false>(four, a.c, mine, top);
+    } else {
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+        if (wave0 + (u + i) * T < g.full) {
+          u4_vec x[1] = {four[i]};
+          if ((int)threadIdx.x + (u + i) * T >= g.full) x[0] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
+          absorb<DT, 1, false, true>(x, a.c, mine, one);
+        }
+    }
+  };
+  const auto group = [&](int u) -> u4_vec(&)[G] { return reinterpret_cast<u4_vec(&)[G]>(w[u]); };
+#pragma unroll
+  for (int u = 0; u < Q; u += G) {
+    sum(group(u), u);
+#pragma unroll
+    for (int i = u; i < u + G; ++i) {
+      room[i][threadIdx.x] = w[i];
+      load((R + i) * T, w[i]);
+    }
+  }
+#pragma unroll
+  for (int u = Q; u < R; u += G) sum(group(u), u);
+#pragma unroll
+  for (int u = 0; u < Q; u += G) sum(group(u), R + u);
+  float top[1];
+  if (last) absorb<DT, 1, false, true>(end, a.c, mine, top);
+  const Stats t = segment_stats<DT, W, false>(g, mine, a.c, sums);
+  if (W == 1) __syncthreads();
+  base.m = t.m;
+  base.less = logf(t.s);
+  const float up = a.inv_t * a.grad[n];
+  const bool empty = t.s == 0.0f, zero = empty || up * head.mass == 0.0f;
+  base.alpha = zero ? 0.0f : up * head.mass;
+  if (threadIdx.x < 64) {
+    float loss = 0.0f;
+    for (int j = threadIdx.x; j < a.k; j += 64)
+      if (list.col[j] >= 0) loss = __builtin_fmaf(expf(list.lp[j]), list.lp[j] - (empty ? kNegInf : (list.w[j] - t.m) * a.inv_t - base.less), loss);
+    loss = wave_sum(loss);
+    if (threadIdx.x == 0) a.loss[n] = loss;
+  }
+  if (zero) {
+    write_base<DT, 4, false, true>(g, out, T, base);
+  } else if (far_maximum(t.m, a.c)) {
+    write_base<DT, 4, false, false>(g, out, T, base);
+  } else {
+    // alpha q = 2^(x c - r) (alpha / S about r): a fused multiply-add, an exp2 and a product to a logit
+    const float r = reference(t.m, a.c), share = base.alpha / t.s * __builtin_amdgcn_exp2f(-__builtin_fmaf(t.m, a.c, -r));
+    const auto turn = [&](const u4_vec& x) {
+      float y[L::V];
+#pragma unroll
+      for (int c = 0; c < L::V; ++c) y[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(L::at(x, c), a.c, -r)) * share;
+      return L::pack(y);
+    };
+    auto* to = out + g.lead;
+    const auto store = [&](int u, const u4_vec& x) {
+      const int i = threadIdx.x + u * T;
+      if (i < g.full) L::store(to + (uint32_t)i * L::V, turn(x));
+    };
+#pragma unroll
+    for (int u = 0; u < R; ++u) store(u < Q ? R + u : u, w[u]);
+#pragma unroll
+    for (int u = 0; u < Q; ++u) store(u, room[u][threadIdx.x]);
+    if (last) {
+      const u4_vec y = turn(end[0]);
+#pragma unroll
+      for (int c = 0; c < L::V; ++c) {
+        typename L::elem v;
+        if constexpr (DT == kF32) v = __uint_as_float(y[c]);
+        else v = (typename L::elem)(y[c / 2] >> (16 * (c & 1)));
+        if (c < g.rest) to[(int64_t)g.full * L::V + c] = v;
+        else if (DT != kF32 && c == L::V - 1 && g.lead != 0) to[-1] = v;
+      }
+    }
+  }
+  __syncthreads();
+  if (empty) return;
+  for (int j = threadIdx.x; j < a.k; j += T)
+    write_entry<DT>(a, list, j, 0, a.M, out, -up, zero ? 0.0f : base.template at<false>(list.w[j]), [&](int i) { return expf(list.lp[i]); });
+}
+
+// The same for rows too wide to hold: the row is read twice, the second time from the caches if it is still there.
 template <int DT, int W>
 __global__ __launch_bounds__(64 * W) void distill_row_kernel(LogitsArgs a) {
   using L = Logits<DT>;
   constexpr int T = 64 * W;
-  __shared__ ListRoom list;
+  extern __shared__ float list_memory[];
+  __shared__ ListHead head;
+  ListRoom list(list_memory, a.k, head);
   __shared__ float4 sums[W];
   const int64_t n = a.row0 + blockIdx.x;
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
@@ -1090,7 +1243,7 @@ __global__ __launch_bounds__(64 * W) void distill_row_kernel(LogitsArgs a) {
   if (threadIdx.x < 64) teacher_list(a, n, list);
   __syncthreads();
   Base base = {0.0f, 0.0f, 0.0f, 0.0f, a.inv_t, 0.0f};
-  if (list.mass == 0.0f) {  // no entry counts: no loss, and a gradient of zero whatever the logits are
+  if (head.mass == 0.0f) {  // no entry counts: no loss, and a gradient of zero whatever the logits are
     if (threadIdx.x == 0) a.loss[n] = 0.0f;
     write_base<DT, 4, false, true>(g, out, T, base);
     return;
@@ -1103,7 +1256,7 @@ __global__ __launch_bounds__(64 * W) void distill_row_kernel(LogitsArgs a) {
     if (threadIdx.x == 0) a.loss[n] = loss;
   }
   const float up = a.inv_t * a.grad[n];
-  base.alpha = up * list.mass;
+  base.alpha = up * head.mass;
   const bool empty = t.s == 0.0f;
   write_gradient<DT, T, false>(a, list, g, 0, a.M, out, base, empty ? 0.0f : -up, empty || base.alpha == 0.0f);
 }

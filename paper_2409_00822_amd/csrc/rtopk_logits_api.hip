@@ -263,7 +263,8 @@ int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dt
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err;
   if (l.segments == 1) {
-    err = sliced(a, [&](int64_t rows) { return rtopk::launch_distill_row(dtype, l.waves, a, rows, s); });
+    const rtopk::HeldLayout h = rtopk::held_layout(M, dtype);
+    err = sliced(a, [&](int64_t rows) { return rtopk::launch_distill_row(dtype, h.waves, h.loads, a, rows, s); });
   } else {
     err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_rows(dtype, rtopk::kOpDistill, l.waves, true, a, rows, s); });
     if (in_place(a) && err == hipSuccess) {

@@ -39,6 +39,7 @@ struct LogitsArgs {
 hipError_t launch_logits_rows(int dtype, int op, int waves, bool split, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 hipError_t launch_logits_join(int dtype, int op, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 hipError_t launch_logits_grad(int dtype, int op, bool join, const LogitsArgs& a, int64_t rows, hipStream_t stream);
-hipError_t launch_distill_row(int dtype, int waves, const LogitsArgs& a, int64_t rows, hipStream_t stream);
+// (waves, loads) of RTOPK_HELD_LIST: the row in registers; loads 0: read twice
+hipError_t launch_distill_row(int dtype, int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 
 }  // namespace rtopk

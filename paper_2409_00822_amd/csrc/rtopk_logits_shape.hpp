@@ -20,6 +20,9 @@ struct LogitsLayout {
   int waves, segments, cols;
 };
 
+// Rows held on chip by one workgroup, X(wavefronts, 128-bit loads of a thread in registers, in LDS), narrow ones first.
+#define RTOPK_HELD_LIST(X) X(1, 4, 0) X(4, 4, 0) X(4, 4, 4) X(8, 4, 4) X(8, 8, 8) X(8, 16, 8) X(8, 24, 8) X(16, 8, 8)
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A workgroup for each row.
@@ -42,6 +45,19 @@ inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   l.segments = (int)ceil_div(M, l.cols);
   l.waves = 4;
   return l.segments > 1 ? l : logits_layout_whole(N, M, k);
+}
+
+struct HeldLayout {
+  int waves, loads;  // loads 0: the row is too wide
+};
+
+inline HeldLayout held_layout(int M, int dtype) {
+  const int64_t chunks = M / logits_width(dtype);  // (a partial one is held apart)
+#define X(w, r, q) \
+  if (chunks <= 64 * w * (r + q) && !(dtype == 0 && w == 8 && r == 24)) return {w, r + q};
+  RTOPK_HELD_LIST(X)
+#undef X
+  return {8, 0};
 }
 
 // The segments of a gradient whose row sums are known.  A gradient that takes its logits' place has one: a row whose log-sum-exp is large is
