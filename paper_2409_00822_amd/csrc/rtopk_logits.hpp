@@ -169,18 +169,13 @@ __device__ __forceinline__ Running block_join(Running t, float c, float4* room) 
   if (W == 1) return t;
   if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = make_float4(t.m, t.s, t.a, 0.0f);
   __syncthreads();
-  float m = room[0].x;
-#pragma unroll
-  for (int w = 1; w < W; ++w) m = fmaxf(m, room[w].x);
-  Running all = {m, 0.0f, 0.0f};
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    Running u = {room[w].x, room[w].y, room[w].z};
-    rise_to<ENT>(u, m, c);
-    all.s += u.s;
-    all.a += u.a;
-  }
-  return all;
+  const int lane = threadIdx.x & 63;  // each wavefront takes them all, one to a lane
+  Running u = {kNegInf, 0.0f, 0.0f};
+  if (lane < W) u = {room[lane].x, room[lane].y, room[lane].z};
+  rise_to<ENT>(u, wave_max(u.m), c);
+  u.s = wave_sum(u.s);
+  if (ENT) u.a = wave_sum(u.a);
+  return u;
 }
 
 // Behind the main path: what seldom follows widens the loads again, rather than that every value is kept for it.
@@ -374,7 +369,8 @@ struct TopRoom {
   static constexpr int kAll = W * kList;
   uint64_t found[W][kList];
   uint64_t best[kMaxAlternatives];
-  uint32_t key[T];
+  static constexpr int kKeys = W == 16 ? T / 4 : T;  // maxima that floors are found among: of four threads where there are many
+  uint32_t key[kKeys];
   int listed[W];
   uint32_t floor;
   int count, reach;
@@ -501,11 +497,17 @@ __device__ __forceinline__ void drop_below(uint32_t least, TopRoom<W>& room, int
 // than -inf.
 template <int W>
 __device__ __forceinline__ float raise_floor(float seen, int k, TopRoom<W>& room) {
-  const uint32_t key = order_key(seen);
-  room.key[threadIdx.x] = key == kLowKey ? 0 : key;
+  uint32_t key = order_key(seen);
+  if (W == 16) {
+    key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xb1, 0xf, 0xf, false));
+    key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4e, 0xf, 0xf, false));
+    if ((threadIdx.x & 3) == 0) room.key[threadIdx.x >> 2] = key == kLowKey ? 0 : key;
+  } else {
+    room.key[threadIdx.x] = key == kLowKey ? 0 : key;
+  }
   __syncthreads();
   if (threadIdx.x < 64) {
-    const uint32_t f = find_floor<64 * W>(room.key, k);
+    const uint32_t f = find_floor<TopRoom<W>::kKeys>(room.key, k);
     if (threadIdx.x == 0) room.floor = f == 0 ? kLowKey + 1 : f;
   }
   __syncthreads();
@@ -889,43 +891,47 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
       v[p] = i < all ? keys[i] : 0;
       top = max(top, (uint32_t)(v[p] >> 32));
     }
-    room.key[threadIdx.x] = top;
     if (threadIdx.x == 0) room.count = 0;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-      const uint32_t f = find_floor<T>(room.key, a.k);
-      if (threadIdx.x == 0) room.floor = f;
-    }
-    __syncthreads();
-    uint64_t least = (uint64_t)max(room.floor, 1u) << 32;  // (0: all that are keys)
-    int n_reach = 0;
-#pragma unroll
-    for (int p = 0; p < P; ++p) n_reach += v[p] >= least;
-    if (n_reach > 0) atomicAdd(&room.count, n_reach);
-    __syncthreads();
-    int reach = room.count;
-    __syncthreads();
-    // more than there is room for: bisection on the whole keys, which are distinct
-    uint64_t b = ~(uint64_t)0;
-    while (reach > TopRoom<4>::kAll) {
-      const uint64_t mid = least + (b - least) / 2;
-      if (threadIdx.x == 0) room.count = 0;
+    uint64_t least = 1;  // any key
+    if (all > 128) {  // (so few are ranked as they are)
+      room.key[threadIdx.x] = top;
       __syncthreads();
-      n_reach = 0;
-#pragma unroll
-      for (int p = 0; p < P; ++p) n_reach += v[p] >= mid;
-      if (n_reach > 0) atomicAdd(&room.count, n_reach);
-      __syncthreads();
-      const int got = room.count;
-      __syncthreads();
-      if (got >= a.k) {
-        least = mid;
-        reach = got;
-      } else {
-        b = mid;
+      if (threadIdx.x < 64) {
+        const uint32_t f = find_floor<T>(room.key, a.k);
+        if (threadIdx.x == 0) room.floor = f;
       }
+      __syncthreads();
+      least = (uint64_t)max(room.floor, 1u) << 32;  // (0: all that are keys)
     }
-    if (threadIdx.x == 0) room.count = 0;
+    if (all > TopRoom<4>::kAll) {
+      // bisection on the whole keys, which are distinct, where more reach the floor than there is room for
+      int reach = all;
+      const auto count = [&](uint64_t mid) {
+        if (threadIdx.x == 0) room.count = 0;
+        __syncthreads();
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < P; ++p) n += v[p] >= mid;
+        if (n > 0) atomicAdd(&room.count, n);
+        __syncthreads();
+        n = room.count;
+        __syncthreads();
+        return n;
+      };
+      reach = count(least);
+      uint64_t b = ~(uint64_t)0;
+      while (reach > TopRoom<4>::kAll) {
+        const uint64_t mid = least + (b - least) / 2;
+        const int n = count(mid);
+        if (n >= a.k) {
+          least = mid;
+          reach = n;
+        } else {
+          b = mid;
+        }
+      }
+      if (threadIdx.x == 0) room.count = 0;
+    }
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < P; ++p)

@@ -25,19 +25,24 @@ struct LogitsLayout {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A workgroup for each row.
+// Few wide rows are spread over workgroups, in two launches: below 96 rows of more than 128 KiB (64 x 131072 bfloat16: 9.9 us against 10.8, with 20
+// alternatives 16.0 against 20.0; 200 rows of them 16.5 against 12.4, 27.5 against 21.5), of more than 64 KiB where more than 8 alternatives
+// are looked for (33 x 32000 fp32, k = 20: 12.3 against 13.8; k = 5 11.0 against 10.8).
+inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > (k > 8 ? 65536 : 131072); }
+
+// A workgroup for each row: a wavefront for short rows; sixteen for few rows, four for more of them (400 x 32000 bfloat16: 11.7 against 8.9 us, 200 x 32000
+// fp32 7.9 against 9.6).
 inline LogitsLayout logits_layout_whole(int64_t N, int M, int k) {
-  return {M <= 2048 && k <= 32 ? 1 : (N <= 256 ? 16 : 4), 1, M};
+  return {M <= 2048 && k <= 32 ? 1 : (N <= 320 ? 16 : 4), 1, M};
 }
 
 inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   const int v = logits_width(dtype);
   const int64_t bytes = (int64_t)M * (dtype == 0 ? 4 : 2);
-  int64_t segments = 1;
-  if (N < 512) {
-    segments = ceil_div(1024, N);
-    if (segments > ceil_div(bytes, 16384)) segments = ceil_div(bytes, 16384);
-  }
+  if (!spread(N, bytes, k)) return logits_layout_whole(N, M, k);
+  // segments of 16 KiB, fewer where that makes more workgroups than fill the GPU four times
+  int64_t segments = ceil_div(1024, N);
+  if (segments > ceil_div(bytes, 16384)) segments = ceil_div(bytes, 16384);
   if (segments > kMaxLogitsSegments) segments = kMaxLogitsSegments;
   if (k > 0 && segments * k > kMaxMergeKeys) segments = kMaxMergeKeys / k;
   LogitsLayout l;
@@ -60,12 +65,13 @@ inline HeldLayout held_layout(int M, int dtype) {
   return {8, 0};
 }
 
-// The segments of a gradient whose row sums are known.  A gradient that takes its logits' place has one: a row whose log-sum-exp is large is
+// The segments of a gradient whose row sums are known: 16 KiB (4096 x 131072 bfloat16: 340 us; 8 KiB 395, 32 KiB 350), less, down to 4 KiB, where
+// that leaves compute units without work.  A gradient that takes its logits' place has one: a row whose log-sum-exp is large is
 // read whole before any of it is written.
 inline LogitsLayout logits_grad_layout(int64_t N, int M, int dtype, bool in_place) {
   if (in_place) return {4, 1, M};
   const int v = logits_width(dtype);
-  int64_t cols = 32768 / (dtype == 0 ? 4 : 2);
+  int64_t cols = 16384 / (dtype == 0 ? 4 : 2);
   while (cols > 1024 * v / 4 && N * ceil_div(M, cols) < 1024) cols /= 2;
   LogitsLayout l;
   l.segments = (int)ceil_div(M, cols);
