@@ -223,7 +223,8 @@ int64_t rtopk_logits_workspace_bytes(int64_t N, int32_t M, int32_t dtype, int32_
  *   k                : alternatives of each row, 0 <= k <= min(128, M).
  *   out_logprobs     : [N][G] fp32, ln q at the tokens (NULL where G is 0).
  *   out_entropy      : [N] fp32, -sum_v q_v ln q_v (optional).
- *   out_lse          : [N] fp32 (optional); the backward call takes it.
+ *   out_lse          : [N] fp32 (optional); the backward call takes it.  Finite unless the row has nothing but -inf, a NaN or +inf (beyond fp32: its last
+ *                      finite number).
  *   out_top_logprobs : [N][k] fp32, ln q of the k largest logits, largest first; equal logits by ascending column (NULL where k is 0).
  *   out_top_cols     : [N][k] int32_t, their columns (NULL where k is 0).
  */

@@ -147,7 +147,10 @@ __device__ __forceinline__ void scale_to(Stats& t, float m, float c) {
 struct Running {
   float m, s, a;
 };
-__device__ __forceinline__ float reference(float m, float c) { return fmaxf(m * c, -1e37f); }
+// Rounding moves r by up to 2^-24 of it, which is small against 1 up to kFarReference; maxima below stay above their reference's place so that no term
+// overflows, and a segment whose maximum lies beyond is summed again (segment_stats).
+constexpr float kFarReference = 1048576.0f;
+__device__ __forceinline__ float reference(float m, float c) { return fmaxf(m * c, -kFarReference); }
 
 template <bool ENT>
 __device__ __forceinline__ void rise_to(Running& t, float m, float c) {
@@ -157,8 +160,8 @@ __device__ __forceinline__ void rise_to(Running& t, float m, float c) {
   t.m = m;
 }
 
-// Whether differences from m c say nothing.
-__device__ __forceinline__ bool far_maximum(float m, float c) { return fabsf(m * c) >= 1e37f && fabsf(m) < __builtin_inff(); }
+// Whether differences from m c are too coarse: a row of nothing but a mask's large negative value, a very low temperature.
+__device__ __forceinline__ bool far_maximum(float m, float c) { return fabsf(m * c) > kFarReference && fabsf(m) < __builtin_inff(); }
 
 // All W wavefronts' sums, in every thread.  `room`: W entries; a barrier lies between its writes and reads.
 template <int W, bool ENT>
@@ -325,7 +328,7 @@ template <int DT, int W, bool ENT>
 __device__ __forceinline__ Stats segment_stats(const Segment<DT>& g, const Running& mine, float c, float4* room) {
   const Running t = block_join<W, ENT>(mine, c, room);
   if (far_maximum(t.m, c)) {
-    // m c is no number to take differences from (a row of nothing but the type's lowest value, a very low temperature): x - m is
+    // x - m is exact or nearly so
     Stats u = {t.m, 0.0f, 0.0f};
     for (int i = threadIdx.x; i < g.chunks(); i += 64 * W)
       g.each(i, [&](int, float x) {
@@ -759,6 +762,13 @@ __device__ __forceinline__ void token_list(const LogitsArgs& a, int64_t n, ListR
   }
 }
 
+// -inf for a row of nothing but -inf, and for no other: what lies beyond fp32 is its last finite number.
+__device__ __forceinline__ float log_sum_exp(const LogitsArgs& a, const Stats& t, float ln_s) {
+  if (t.s == 0.0f) return kNegInf;
+  const float v = __builtin_fmaf(t.m, a.inv_t, ln_s);
+  return fabsf(v) == __builtin_inff() && fabsf(t.m) < __builtin_inff() ? copysignf(3.402823466e38f, v) : v;
+}
+
 // Loss of the row from its list; the first wavefront's work, in its every lane.
 template <int DT>
 __device__ __forceinline__ float list_loss(const LogitsArgs& a, const typename Logits<DT>::elem* row, const Stats& t, float ln_s, const ListRoom& r) {
@@ -784,7 +794,7 @@ __device__ __forceinline__ void write_tokens(const LogitsArgs& a, int64_t n, con
     a.logprobs[n * a.tokens_per_row + g] = lp;
   }
   if (threadIdx.x == 0) {
-    if (a.lse) a.lse[n] = empty ? kNegInf : __builtin_fmaf(t.m, a.inv_t, ln_s);
+    if (a.lse) a.lse[n] = log_sum_exp(a, t, ln_s);
     if (a.entropy) a.entropy[n] = empty ? 0.0f : ln_s - t.a / t.s * a.inv_t;
   }
 }
@@ -839,7 +849,7 @@ __global__ __launch_bounds__(64 * W) void logits_rows_kernel(LogitsArgs a) {
     const float ln_s = logf(t.s), loss = list_loss<DT>(a, row, t, ln_s, list);
     if (threadIdx.x == 0) {
       a.loss[n] = loss;
-      if (a.lse) a.lse[n] = t.s == 0.0f ? kNegInf : __builtin_fmaf(t.m, a.inv_t, ln_s);
+      if (a.lse) a.lse[n] = log_sum_exp(a, t, ln_s);
     }
   }
 }
@@ -948,7 +958,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
     const float loss = list_loss<DT>(a, row, t, ln_s, list);
     if (threadIdx.x == 0) {
       a.loss[n] = loss;
-      if (a.lse) a.lse[n] = t.s == 0.0f ? kNegInf : __builtin_fmaf(t.m, a.inv_t, ln_s);
+      if (a.lse) a.lse[n] = log_sum_exp(a, t, ln_s);
     }
   }
 }

@@ -53,7 +53,9 @@ def rows(N, M, dtype, seed, pad=0, shift=0, scale=3.0, mask=None):
 def near(got, want, tol, what):
     got, want = np.asarray(got, dtype=np.float64), np.asarray(want, dtype=np.float64)
     tol = np.broadcast_to(tol, want.shape)
-    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    # a value beyond fp32 is its last finite number or infinite
+    last = float(np.finfo(np.float32).max)
+    same = (got == want) | (np.isnan(got) & np.isnan(want)) | ((np.abs(want) + tol >= last) & (np.sign(got) == np.sign(want)) & (np.abs(got) >= last * (1 - 2.0**-23)))
     with np.errstate(invalid="ignore"):
         ok = same | (np.abs(got - want) <= tol)
     assert ok.all(), f"{what}: {np.argwhere(~ok)[:3].tolist()} got {got[~ok][:3]} want {want[~ok][:3]} tol {tol[~ok][:3]}"

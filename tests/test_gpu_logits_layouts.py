@@ -99,3 +99,17 @@ def test_large_log_sum_exps(dtype):
         want = R.rtopk_token_logprobs_backward(g, x, t, lse, 0.25)
         y = x.clone()
         assert torch.equal(R.rtopk_token_logprobs_backward(g, y, t, lse, 0.25, grad_logits=y), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [-1e4, -1e9, -1e20, -1e30])
+@pytest.mark.parametrize("keep", [0.0, 0.002, 0.5])
+def test_masks_of_large_negative_values(value, keep, dtype):
+    R = _gpu()
+    mask = lambda x, g: x.masked_fill_(torch.rand(x.shape, generator=g) >= keep, value)  # noqa: E731
+    for N, M in ((3, 1500), (3, 30000), (3, 90000), (330, 2300)):
+        x, xh = rows(N, M, dtype, seed=M, mask=mask)
+        for k in (0, 20):
+            check_forward(R, x, xh, some_tokens(N, M, 1, 1), k)
+        check_token_gradient(R, x, xh, some_tokens(N, M, 1, 1), 1.0, True, 3, dtype)
+        check_distill(R, x, xh, teacher_list(N, M, 20, 3), 1.0, False, dtype, 3)
