@@ -25,21 +25,22 @@ struct LogitsLayout {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Few wide rows are spread over workgroups, in two launches: below 96 rows of more than 128 KiB (64 x 131072 bfloat16: 9.9 us against 10.8, with 20
-// alternatives 16.0 against 20.0; 200 rows of them 16.5 against 12.4, 27.5 against 21.5), of more than 64 KiB where more than 8 alternatives
-// are looked for (33 x 32000 fp32, k = 20: 12.3 against 13.8; k = 5 11.0 against 10.8).
-inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > (k > 8 ? 65536 : 131072); }
+// Few rows of more than 128 KiB are spread over several workgroups each, in two launches, unless the alternatives' merge costs more than that saves:
+// 8 x 131072 bfloat16 without alternatives 8.9 us against 10.0 in one workgroup, with 20 12.7 against 15.6, with 64 30.5 against 22.5; 96 rows 12.8
+// against 11.2; 64 x 32000 fp32, k = 20, 13.4 against 10.0.
+inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > 131072 && k <= 32; }
 
-// A workgroup for each row: a wavefront for short rows; sixteen for few rows, four for more of them (400 x 32000 bfloat16: 11.7 against 8.9 us, 200 x 32000
-// fp32 7.9 against 9.6).
-inline LogitsLayout logits_layout_whole(int64_t N, int M, int k) {
-  return {M <= 2048 && k <= 32 ? 1 : (N <= 320 ? 16 : 4), 1, M};
+// A workgroup for each row: one wavefront for short rows; sixteen where there are no more rows than compute units, or twice as many wide ones; else four
+// (300 x 32000 bfloat16, k = 5: 15.9 us with sixteen, 14.2 with four; 200 x 131072 19.3 against 29.2, 400 29.8 against 33.2, 1000 x 32000 fp32 45 against 26).
+inline LogitsLayout logits_layout_whole(int64_t N, int M, int dtype, int k) {
+  const bool wide = (int64_t)M * (dtype == 0 ? 4 : 2) > 131072;
+  return {M <= 2048 && k <= 32 ? 1 : (N <= (wide ? 512 : 256) ? 16 : 4), 1, M};
 }
 
 inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   const int v = logits_width(dtype);
   const int64_t bytes = (int64_t)M * (dtype == 0 ? 4 : 2);
-  if (!spread(N, bytes, k)) return logits_layout_whole(N, M, k);
+  if (!spread(N, bytes, k)) return logits_layout_whole(N, M, dtype, k);
   // segments of 16 KiB, fewer where that makes more workgroups than fill the GPU four times
   int64_t segments = ceil_div(1024, N);
   if (segments > ceil_div(bytes, 16384)) segments = ceil_div(bytes, 16384);
@@ -49,7 +50,7 @@ inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   l.cols = (int)(ceil_div(ceil_div(M, segments), v) * v);
   l.segments = (int)ceil_div(M, l.cols);
   l.waves = 4;
-  return l.segments > 1 ? l : logits_layout_whole(N, M, k);
+  return l.segments > 1 ? l : logits_layout_whole(N, M, dtype, k);
 }
 
 struct HeldLayout {
