@@ -269,7 +269,8 @@ int rtopk_distill_backward(const float* grad_loss, const void* logits, int32_t d
 
 /*
  * Both at once, for weights [N] that are known before the loss is (1 / N for a mean): out_loss as rtopk_distill's, not weighted, grad_logits as
- * rtopk_distill_backward's for grad_loss = weights.  Rows without an entry that counts are not read.
+ * rtopk_distill_backward's for grad_loss = weights.  Rows of up to 256 KiB are read once (few of more than 128 KiB, which are spread, twice), wider ones
+ * twice.  A row without an entry that counts has loss 0 and gradient 0 whatever its logits are.
  */
 int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride,
                             const void* teacher_vals, int32_t teacher_dtype, const int32_t* teacher_cols, int32_t k, int32_t log_probs,

@@ -37,7 +37,6 @@ typedef u4_vec u4_word __attribute__((aligned(4)));
 template <int DT>
 struct Logits {
   static constexpr int V = DT == kF32 ? 4 : 8;  // values of a 128-bit load
-  static constexpr int B = DT == kF32 ? 4 : 2;  // bytes of one
   using elem = typename std::conditional<DT == kF32, float, uint16_t>::type;
   using any4 = typename std::conditional<DT == kF32, u4_word, u4_half>::type;
   static constexpr uint32_t kLow = DT == kF32 ? 0xff800000u : (DT == kF16 ? 0xfc00fc00u : 0xff80ff80u);  // -inf
@@ -370,7 +369,7 @@ struct TopRoom {
   static constexpr int T = 64 * W;
   static constexpr int kList = W == 1 ? 512 : (W == 4 ? 256 : 128);  // of a wavefront
   static constexpr int kAll = W * kList;
-  uint64_t found[W][kList];
+  uint64_t found[kAll];  // the wavefronts' lists, one behind the other
   uint64_t best[kMaxAlternatives];
   static constexpr int kKeys = W == 16 ? T / 4 : T;  // maxima that floors are found among: of four threads where there are many
   uint32_t key[kKeys];
@@ -441,7 +440,7 @@ __device__ __forceinline__ void rank_listed(TopRoom<W>& room, int k) {
   for (int j = all + threadIdx.x; j < k; j += 64 * W) room.best[j] = 0;
   if (all <= 64) {  // a key to a lane of the first wavefront, each held against all by way of scalar registers
     if (wave == 0) {
-      const uint64_t key = lane < all ? room.found[0][at] : 0;
+      const uint64_t key = lane < all ? room.found[at] : 0;
       int rank = 0;
       for (int i = 0; i < all; ++i) {
         const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, i);
@@ -452,12 +451,12 @@ __device__ __forceinline__ void rank_listed(TopRoom<W>& room, int k) {
   } else {
     const int n = room.listed[wave];
     for (int j = lane; j < n; j += 64) {
-      const uint64_t key = room.found[wave][j];
+      const uint64_t key = room.found[wave * TopRoom<W>::kList + j];
       int rank = 0;
       for (int w = 0; w < W; ++w) {
         const int m = room.listed[w];
 #pragma unroll 8
-        for (int i = 0; i < m; ++i) rank += room.found[w][i] > key;
+        for (int i = 0; i < m; ++i) rank += room.found[w * TopRoom<W>::kList + i] > key;
       }
       if (rank < k) room.best[rank] = key;
     }
@@ -484,7 +483,7 @@ __device__ __forceinline__ int count_reaching(const Segment<DT>& g, uint32_t lea
 template <int DT, int W, typename F>
 __device__ __forceinline__ void list_chunk(const u4_vec& w, float floor, TopRoom<W>& room, int& n, F col) {
   using L = Logits<DT>;
-  uint64_t* list = room.found[threadIdx.x >> 6];
+  uint64_t* list = room.found + (threadIdx.x >> 6) * TopRoom<W>::kList;
   u4_vec here = w;
   asm volatile("" : "+v"(here));  // (else all loads are widened before the branch)
 #pragma unroll
@@ -502,7 +501,7 @@ __device__ __forceinline__ void list_chunk(const u4_vec& w, float floor, TopRoom
 // Drops what lies below the floor from the wavefront's list.
 template <int W>
 __device__ __forceinline__ void drop_below(uint32_t least, TopRoom<W>& room, int& n) {
-  uint64_t* list = room.found[threadIdx.x >> 6];
+  uint64_t* list = room.found + (threadIdx.x >> 6) * TopRoom<W>::kList;
   const int lane = threadIdx.x & 63;
   int kept = 0;
   for (int i = 0; i < n; i += 64) {
@@ -538,7 +537,7 @@ __device__ __forceinline__ float raise_floor(float seen, int k, TopRoom<W>& room
 // The first columns whose key is `least` follow the n of the first list up to k; the first wavefront's work.  Returns how many there are then.
 template <int DT, int W>
 __device__ int fill_list(const Segment<DT>& g, int first, int k, uint32_t least, int n, TopRoom<W>& room) {
-  uint64_t* list = room.found[0];
+  uint64_t* list = room.found;
   const int lane = threadIdx.x, chunks = g.chunks();
   if (g.lead != 0 && n < k && order_key(Logits<DT>::widen(g.body[-1])) == least) {
     if (lane == 0) list[n] = place_key(least, first);
@@ -598,7 +597,7 @@ __device__ void list_again(const Segment<DT>& g, int first, int k, uint32_t leas
         const uint32_t o = order_key(v);
         if (o >= listed) {
           const int at = atomicAdd(&room.count, 1);
-          if (at < kAll) room.found[0][at] = place_key(o, first + col);  // (the lists follow one another)
+          if (at < kAll) room.found[at] = place_key(o, first + col);  // (the lists follow one another)
         }
       });
   __syncthreads();
@@ -628,6 +627,7 @@ __device__ Running stats_and_top(const Segment<DT>& g, int first, int k, float c
   const auto raise = [&] {
     floor = raise_floor<W>(t.m, k, room);
     lost |= n > kList;
+    n = min(n, kList);
     drop_below<W>(order_key(floor), room, n);
   };
   const auto list = [&](const u4_vec(&w)[U], const float(&top)[U], int b) {
@@ -641,7 +641,7 @@ __device__ Running stats_and_top(const Segment<DT>& g, int first, int k, float c
   u4_vec w[U];
   float top[U];
   const int batches = g.full / (U * T);
-  constexpr bool AHEAD = W == 16;  // few rows: nothing else covers the wait for the next batch
+  constexpr bool AHEAD = W == 16 && U == 4;  // few rows: nothing else covers the wait for the next batch (eight loads have no registers left for it)
   if (AHEAD && batches > 0) load_batch<DT, T, U, false>(g, 0, w);
   for (int b = 0; b < batches; ++b) {
     u4_vec next[U];
@@ -708,7 +708,7 @@ __device__ __forceinline__ float teacher_at(const LogitsArgs& a, int64_t i) {
 __device__ __forceinline__ bool any_entry(const LogitsArgs& a, int64_t n) {
   for (int j = threadIdx.x & 63; j - (int)(threadIdx.x & 63) < a.k; j += 64) {
     const int col = j < a.k ? a.teacher_cols[n * a.k + j] : -1;
-    if (__any(col >= 0 && col < a.M && teacher_at(a, n * a.k + j) > kNegInf)) return true;
+    if (__any(col >= 0 && col < a.M && !(teacher_at(a, n * a.k + j) == kNegInf))) return true;  // (NaN counts)
   }
   return false;
 }
@@ -972,7 +972,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if (v[p] >= least) room.found[0][atomicAdd(&room.count, 1)] = v[p];
+      if (v[p] >= least) room.found[atomicAdd(&room.count, 1)] = v[p];
     __syncthreads();
     set_listed(room, room.count);
     __syncthreads();

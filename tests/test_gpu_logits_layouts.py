@@ -113,3 +113,21 @@ def test_masks_of_large_negative_values(value, keep, dtype):
             check_forward(R, x, xh, some_tokens(N, M, 1, 1), k)
         check_token_gradient(R, x, xh, some_tokens(N, M, 1, 1), 1.0, True, 3, dtype)
         check_distill(R, x, xh, teacher_list(N, M, 20, 3), 1.0, False, dtype, 3)
+
+
+def test_a_teacher_of_nan_spoils_its_row_only():
+    """Alike in all forms: NaN loss and gradient, and only there."""
+    R = _gpu()
+    for N, M in ((5, 3000), (5, 70000), (5, 140001), (600, 2500)):
+        x, _ = rows(N, M, "f32", seed=1)
+        vals, cols, _, _ = teacher_list(N, M, 6, 2, spoil=False)
+        vals[1] = float("nan")
+        vals[3, 2] = float("nan")
+        w = torch.ones(N, device="cuda")
+        loss, lse = R.rtopk_distill(x, vals, cols)
+        loss2, dx = R.rtopk_distill_with_grad(w, x, vals, cols)
+        dx2 = R.rtopk_distill_backward(w, x, vals, cols, lse)
+        bad = torch.zeros(N, dtype=torch.bool, device="cuda")
+        bad[1] = bad[3] = True
+        for o in (loss, loss2, dx.sum(1), dx2.sum(1)):
+            assert torch.equal(torch.isnan(o), bad)
