@@ -13,6 +13,7 @@ hipError_t rows_of(int waves, bool split, const LogitsArgs& a, int64_t rows, hip
   switch (waves) {
     case 1: return launch_kernel(logits_rows_kernel<DT, 1, OP, TOP, false>, grid, dim3(64), lds, s, a);
     case 4: return launch_kernel(logits_rows_kernel<DT, 4, OP, TOP, false>, grid, dim3(256), lds, s, a);
+    case 8: return launch_kernel(logits_rows_kernel<DT, 8, OP, TOP, false>, grid, dim3(512), lds, s, a);
     default: return launch_kernel(logits_rows_kernel<DT, 16, OP, TOP, false>, grid, dim3(1024), lds, s, a);
   }
 }

@@ -227,7 +227,7 @@ __device__ __forceinline__ void absorb(u4_vec (&w)[U], float c, Running& t, floa
 
 // `cols` columns from `row` on, in chunks of a load's width; chunk i belongs to thread i mod T.  Rows of 16-bit values that start at an odd one
 // have their first column (`lead`) apart, so that all loads start at multiples of four bytes: from there they run at the rate of aligned ones
-// (8191 x 50001 half: 174 -> 135 us).  What is left at the end (`rest`, less than a chunk) and the lead make up the last chunk.
+// (8191 x 50001 half: 174 -> 131 us).  What is left at the end (`rest`, less than a chunk) and the lead make up the last chunk.
 template <int DT>
 struct Segment {
   using L = Logits<DT>;
@@ -371,7 +371,7 @@ struct TopRoom {
   static constexpr int kAll = W * kList;
   uint64_t found[kAll];  // the wavefronts' lists, one behind the other
   uint64_t best[kMaxAlternatives];
-  static constexpr int kKeys = W == 16 ? T / 4 : T;  // maxima that floors are found among: of four threads where there are many
+  static constexpr int kKeys = W > 4 ? 256 : T;  // maxima that floors are found among: of two or four threads where there are many
   uint32_t key[kKeys];
   int listed[W];
   uint32_t floor;
@@ -518,13 +518,10 @@ __device__ __forceinline__ void drop_below(uint32_t least, TopRoom<W>& room, int
 template <int W>
 __device__ __forceinline__ float raise_floor(float seen, int k, TopRoom<W>& room) {
   uint32_t key = order_key(seen);
-  if (W == 16) {
-    key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xb1, 0xf, 0xf, false));
-    key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4e, 0xf, 0xf, false));
-    if ((threadIdx.x & 3) == 0) room.key[threadIdx.x >> 2] = key == kLowKey ? 0 : key;
-  } else {
-    room.key[threadIdx.x] = key == kLowKey ? 0 : key;
-  }
+  constexpr int of = W > 4 ? W / 4 : 1;
+  if (of >= 2) key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xb1, 0xf, 0xf, false));
+  if (of == 4) key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4e, 0xf, 0xf, false));
+  if (threadIdx.x % of == 0) room.key[threadIdx.x / of] = key == kLowKey ? 0 : key;
   __syncthreads();
   if (threadIdx.x < 64) {
     const uint32_t f = find_floor<TopRoom<W>::kKeys>(room.key, k);
@@ -836,8 +833,13 @@ __device__ __forceinline__ void write_top(const LogitsArgs& a, int64_t n, const 
 
 // One workgroup reads a segment of a row.  SPLIT: its sums and alternatives go to scratch memory for logits_join_kernel; else the segment is the
 // row and the results are written.
+// Many rows: four wavefronts to a row (eight rows to a compute unit, so that some load while others search), bound by HBM for fp32 (8191 x 50000 250 us,
+// 6.55 TB/s; 255 with 20 alternatives), by HBM and the vector ALU in 16 bits, which have twice the terms to a byte (bfloat16 127 us, 6.46 TB/s, its
+// ALU 84 % busy; 154 with 20 alternatives; half, odd columns, one alternative 146).  The bfloat16 form with alternatives is held to 80
+// registers, six wavefronts to a SIMD: 8191 x 50000, k = 20, 164 -> 154 us.  Few rows: bound by the chain load, sums, floor, ranks, each a
+// microsecond or two (1 x 32768 fp32, k = 5, 6.9 us).
 template <int DT, int W, int OP, bool TOP, bool SPLIT>
-__global__ __launch_bounds__(64 * W) void logits_rows_kernel(LogitsArgs a) {
+__global__ __launch_bounds__(64 * W, TOP && W == 4 && DT == kBF16 ? 6 : 1) void logits_rows_kernel(LogitsArgs a) {
   using L = Logits<DT>;
   constexpr int T = 64 * W;
   constexpr bool ENT = OP == kOpTokens;
@@ -900,6 +902,8 @@ __device__ __forceinline__ Stats join_segments(const LogitsArgs& a, int64_t n, f
   return t;
 }
 
+// Joins a row's segments.  Its time is that of a launch and a few trips to memory, 3.5 to 5 us; a row's last workgroup cannot do the work instead, for
+// the counter that would tell it is the last has to be zero beforehand, which is a launch too.
 template <int DT, int OP, bool TOP>
 __global__ __launch_bounds__(256) void logits_join_kernel(LogitsArgs a) {
   using L = Logits<DT>;
@@ -1094,6 +1098,8 @@ __device__ __forceinline__ void write_gradient(const LogitsArgs& a, const ListRo
   write_list<DT, T, ENT, false>(a, r, first, cols, out, base, factor, x);
 }
 
+// Bound by HBM: logits read once, gradient written once (4096 x 131072 bfloat16, an eighth of the rows not read, 339 us, 5.95 TB/s; 2048 x 65536 fp32,
+// lists of 100, 172 us, 6.24 TB/s; this repository's copy kernels reach 6.2 to 6.5).
 // A segment of a row's gradient by one workgroup.  The row's sums are known: its log-sum-exp was saved (JOIN false), or the segments' sums
 // lie in scratch memory (JOIN, distillation only), and then the loss is written too.
 template <int DT, int OP, bool ENT, bool JOIN>
@@ -1151,6 +1157,10 @@ __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
 // registers and, for the widest rows, Q more in LDS.  The first Q loads go on to LDS once they are in the sums, and their registers take
 // the last Q.  With eight wavefronts and 128 registers each, two such workgroups share a compute unit, and one's loads and stores overlap
 // the other's arithmetic.
+// Bound by HBM where rows are wide: 8192 x 131072 bfloat16, lists of 64, an eighth of the rows without entries, 750 us (5.38 TB/s; the streaming gradient
+// kernel above takes 762 for all rows' bytes), 4096 x 65536 fp32 380 us (5.65 TB/s), against 930 and 471 us with the row read twice; 2048 x 50000
+// fp32, lists of 100, 167 us (147).  Few rows in flight are better than many: 64 KiB rows on 8 wavefronts of 4 + 4 loads 103 us, on 4 of 16 107; 128 KiB
+// ones on 8 of 8 + 8 381, on 4 of 24 + 8 405.  Workgroups that stay and load their next row while they store one lose 20 to 30 %.
 template <int DT, int W, int R, int Q>
 __global__ __launch_bounds__(64 * W, R + Q > 16 && W == 8 ? 4 : 1) void distill_held_kernel(LogitsArgs a) {
   using L = Logits<DT>;

@@ -60,7 +60,7 @@ inline uint64_t rows_bytes(int64_t N, int32_t M, int64_t stride, int dtype) {
 // The layout of the rows' pass, spread over workgroups only where there is memory for the parts.
 rtopk::LogitsLayout lay_out(LogitsArgs& a, int dtype, int k, void* workspace, int64_t workspace_bytes) {
   rtopk::LogitsLayout l = rtopk::logits_layout(a.N, a.M, dtype, k);
-  if (l.segments > 1 && (!workspace || workspace_bytes < rtopk::logits_workspace(a.N, l, k))) l = rtopk::logits_layout_whole(a.N, a.M, dtype, k);
+  if (l.segments > 1 && (!workspace || workspace_bytes < rtopk::logits_workspace(a.N, l, k))) l = rtopk::logits_layout_whole(a.N, a.M, k);
   a.segments = l.segments;
   a.seg_cols = l.cols;
   a.part = static_cast<float4*>(workspace);

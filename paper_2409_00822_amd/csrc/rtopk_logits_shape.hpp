@@ -30,17 +30,17 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // against 11.2; 64 x 32000 fp32, k = 20, 13.4 against 10.0.
 inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > 131072 && k <= 32; }
 
-// A workgroup for each row: one wavefront for short rows; sixteen where there are no more rows than compute units, or twice as many wide ones; else four
-// (300 x 32000 bfloat16, k = 5: 15.9 us with sixteen, 14.2 with four; 200 x 131072 19.3 against 29.2, 400 29.8 against 33.2, 1000 x 32000 fp32 45 against 26).
-inline LogitsLayout logits_layout_whole(int64_t N, int M, int dtype, int k) {
-  const bool wide = (int64_t)M * (dtype == 0 ? 4 : 2) > 131072;
-  return {M <= 2048 && k <= 32 ? 1 : (N <= (wide ? 512 : 256) ? 16 : 4), 1, M};
+// A workgroup for each row: one wavefront for short rows; sixteen where there are no more rows than compute units, eight up to twice as many, four beyond
+// (k = 5, bfloat16 rows of 131072 columns with 16, 8 and 4 wavefronts: 200 rows 16.2, 20.6 and 29.6 us, 400 30.2, 26.0 and 32.7, 700 44.8, 41.8 and
+// 38.2; without alternatives 200 12.8, 13.7 and 19.9, 400 23.5, 21.9 and 22.7, 700 35.8, 35.1 and 32.3).
+inline LogitsLayout logits_layout_whole(int64_t N, int M, int k) {
+  return {M <= 2048 && k <= 32 ? 1 : (N <= 256 ? 16 : (N <= 512 ? 8 : 4)), 1, M};
 }
 
 inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   const int v = logits_width(dtype);
   const int64_t bytes = (int64_t)M * (dtype == 0 ? 4 : 2);
-  if (!spread(N, bytes, k)) return logits_layout_whole(N, M, dtype, k);
+  if (!spread(N, bytes, k)) return logits_layout_whole(N, M, k);
   // segments of 16 KiB, fewer where that makes more workgroups than fill the GPU four times
   int64_t segments = ceil_div(1024, N);
   if (segments > ceil_div(bytes, 16384)) segments = ceil_div(bytes, 16384);
@@ -50,7 +50,7 @@ inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
   l.cols = (int)(ceil_div(ceil_div(M, segments), v) * v);
   l.segments = (int)ceil_div(M, l.cols);
   l.waves = 4;
-  return l.segments > 1 ? l : logits_layout_whole(N, M, dtype, k);
+  return l.segments > 1 ? l : logits_layout_whole(N, M, k);
 }
 
 struct HeldLayout {

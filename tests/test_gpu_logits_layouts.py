@@ -131,3 +131,15 @@ def test_a_teacher_of_nan_spoils_its_row_only():
         bad[1] = bad[3] = True
         for o in (loss, loss2, dx.sum(1), dx2.sum(1)):
             assert torch.equal(torch.isnan(o), bad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("mask", ["none", "few columns left", "none left", "all equal", "four levels", "ascending", "the largest where a few threads read", "a plateau at the end"])
+def test_eight_wavefronts_to_a_row(mask, dtype):
+    R = _gpu()
+    for N, M, k in ((257, 2300, 128), (400, 9001, 20), (512, 20003, 1)):
+        x, xh = rows(N, M, dtype, seed=N + M, mask=MASKS.get(mask))
+        t = some_tokens(N, M, 1, k)
+        got = R.rtopk_token_logprobs(x, t, k)
+        check_forward(R, x[:9], xh[:9], t[:9], k, got=[g[:9] for g in got])
+        check_forward(R, x[-9:], xh[-9:], t[-9:], k, got=[g[-9:] for g in got])

@@ -108,7 +108,7 @@ int main() {
           // every column in one segment, none empty
           if (l.segments < 1 || l.segments > kMaxLogitsSegments || (int64_t)l.segments * l.cols < M || (int64_t)(l.segments - 1) * l.cols >= M) ++bad;
           if (l.segments > 1 && (l.cols % logits_width(dtype) != 0 || l.waves != 4 || l.segments * (k > 0 ? k : 1) > kMaxMergeKeys)) ++bad;
-          if (l.waves != 1 && l.waves != 4 && l.waves != 16) ++bad;
+          if (l.waves != 1 && l.waves != 4 && l.waves != 8 && l.waves != 16) ++bad;
           // the alternatives' search: threads that hold no column, or at least k, or a row that is listed whole
           if (l.waves == 1 && k > 32) ++bad;
           if (logits_workspace(N, l, k) != (l.segments > 1 ? N * l.segments * (16 + 8 * (int64_t)k) : 0)) ++bad;
