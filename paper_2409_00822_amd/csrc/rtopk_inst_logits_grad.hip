@@ -5,14 +5,21 @@ namespace rtopk {
 
 namespace {
 
+template <int DT, int W>
+hipError_t grad_of_waves(int op, const LogitsArgs& a, int64_t rows, hipStream_t s) {
+  const dim3 grid((uint32_t)(rows * a.segments)), block(64 * W);
+  if (op == kOpDistill) return launch_kernel(logits_grad_kernel<DT, kOpDistill, false, false, W>, grid, block, list_bytes(a.k), s, a);
+  return a.grad_entropy ? launch_kernel(logits_grad_kernel<DT, kOpTokens, true, false, W>, grid, block, list_bytes(a.k), s, a)
+                        : launch_kernel(logits_grad_kernel<DT, kOpTokens, false, false, W>, grid, block, list_bytes(a.k), s, a);
+}
+
 template <int DT>
-hipError_t grad_of_type(int op, bool join, const LogitsArgs& a, int64_t rows, hipStream_t s) {
-  const dim3 grid((uint32_t)(rows * a.segments)), block(256);
-  if (op == kOpDistill)
-    return join ? launch_kernel(logits_grad_kernel<DT, kOpDistill, false, true>, grid, block, list_bytes(a.k), s, a)
-                : launch_kernel(logits_grad_kernel<DT, kOpDistill, false, false>, grid, block, list_bytes(a.k), s, a);
-  return a.grad_entropy ? launch_kernel(logits_grad_kernel<DT, kOpTokens, true, false>, grid, block, list_bytes(a.k), s, a)
-                        : launch_kernel(logits_grad_kernel<DT, kOpTokens, false, false>, grid, block, list_bytes(a.k), s, a);
+hipError_t grad_of_type(int op, int waves, bool join, const LogitsArgs& a, int64_t rows, hipStream_t s) {
+  if (join)
+    return launch_kernel(logits_grad_kernel<DT, kOpDistill, false, true, 4>, dim3((uint32_t)(rows * a.segments)), dim3(256), list_bytes(a.k), s, a);
+  if constexpr (DT != kF32)
+    if (waves == 1) return grad_of_waves<DT, 1>(op, a, rows, s);
+  return grad_of_waves<DT, 4>(op, a, rows, s);
 }
 
 template <int DT>
@@ -27,10 +34,10 @@ hipError_t row_of_type(int waves, int loads, const LogitsArgs& a, int64_t rows, 
 
 }  // namespace
 
-hipError_t launch_logits_grad(int dtype, int op, bool join, const LogitsArgs& a, int64_t rows, hipStream_t s) {
-  return dtype == kF32   ? grad_of_type<kF32>(op, join, a, rows, s)
-         : dtype == kF16 ? grad_of_type<kF16>(op, join, a, rows, s)
-                         : grad_of_type<kBF16>(op, join, a, rows, s);
+hipError_t launch_logits_grad(int dtype, int op, int waves, bool join, const LogitsArgs& a, int64_t rows, hipStream_t s) {
+  return dtype == kF32   ? grad_of_type<kF32>(op, waves, join, a, rows, s)
+         : dtype == kF16 ? grad_of_type<kF16>(op, waves, join, a, rows, s)
+                         : grad_of_type<kBF16>(op, waves, join, a, rows, s);
 }
 
 hipError_t launch_distill_row(int dtype, int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t s) {

@@ -1102,14 +1102,14 @@ __device__ __forceinline__ void write_gradient(const LogitsArgs& a, const ListRo
 // lists of 100, 172 us, 6.24 TB/s; this repository's copy kernels reach 6.2 to 6.5).
 // A segment of a row's gradient by one workgroup.  The row's sums are known: its log-sum-exp was saved (JOIN false), or the segments' sums
 // lie in scratch memory (JOIN, distillation only), and then the loss is written too.
-template <int DT, int OP, bool ENT, bool JOIN>
-__global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
+template <int DT, int OP, bool ENT, bool JOIN, int W>
+__global__ __launch_bounds__(64 * W) void logits_grad_kernel(LogitsArgs a) {
   using L = Logits<DT>;
-  constexpr int T = 256;
+  constexpr int T = 64 * W;
   extern __shared__ float list_memory[];
   __shared__ ListHead head;
   ListRoom list(list_memory, a.k, head);
-  __shared__ float4 sums[4];
+  __shared__ float4 sums[W];
   const int seg = (int)(blockIdx.x % (uint32_t)a.segments);
   const int64_t n = a.row0 + blockIdx.x / (uint32_t)a.segments;
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
@@ -1140,7 +1140,7 @@ __global__ __launch_bounds__(256) void logits_grad_kernel(LogitsArgs a) {
     __syncthreads();
     if (fabsf(base.less) > kLargeLse && fabsf(base.less) < __builtin_inff()) {
       const Segment<DT> all(row, a.M);
-      const Stats t = segment_stats<DT, 4, false>(all, thread_stats<DT, T, 4, false, true>(all, a.c), a.c, sums);
+      const Stats t = segment_stats<DT, W, false>(all, thread_stats<DT, T, 4, false, true>(all, a.c), a.c, sums);
       base.m = t.m;
       base.less = logf(t.s);
     }

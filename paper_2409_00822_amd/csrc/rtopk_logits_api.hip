@@ -95,7 +95,7 @@ int backward(LogitsArgs& a, int dtype, int op, void* stream) {
   a.segments = l.segments;
   a.seg_cols = l.cols;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_grad(dtype, op, false, a, rows, s); });
+  const hipError_t err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_grad(dtype, op, l.waves, false, a, rows, s); });
   return err == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;
 }
 
@@ -272,7 +272,7 @@ int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dt
       err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_join(dtype, rtopk::kOpDistill, a, rows, s); });
       a.loss = nullptr;
     }
-    if (err == hipSuccess) err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_grad(dtype, rtopk::kOpDistill, true, a, rows, s); });
+    if (err == hipSuccess) err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_grad(dtype, rtopk::kOpDistill, l.waves, true, a, rows, s); });
   }
   return err == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;
 }

@@ -38,7 +38,7 @@ struct LogitsArgs {
 // Each enqueues its kernel for rows [a.row0, a.row0 + rows); dtype: of the logits.
 hipError_t launch_logits_rows(int dtype, int op, int waves, bool split, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 hipError_t launch_logits_join(int dtype, int op, const LogitsArgs& a, int64_t rows, hipStream_t stream);
-hipError_t launch_logits_grad(int dtype, int op, bool join, const LogitsArgs& a, int64_t rows, hipStream_t stream);
+hipError_t launch_logits_grad(int dtype, int op, int waves, bool join, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 // (waves, loads) of RTOPK_HELD_LIST: the row in registers; loads 0: read twice
 hipError_t launch_distill_row(int dtype, int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t stream);
 

@@ -30,11 +30,15 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // against 11.2; 64 x 32000 fp32, k = 20, 13.4 against 10.0.
 inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > 131072 && k <= 32; }
 
+// Rows that one wavefront takes: up to 2048 columns, and up to 16384 where there are rows enough to fill the GPU so, which pays no barriers (16384 x 4000
+// bfloat16 36 -> 25 us, with 5 alternatives 62 -> 39; 8192 x 16000, 5 alternatives 64 -> 56; 1000 x 4000, 5 alternatives 8.1 against 9.4).
+inline bool short_rows(int64_t N, int M, int k) { return k <= 32 && (M <= 2048 || (M <= 16384 && N >= 4096)); }
+
 // A workgroup for each row: one wavefront for short rows; sixteen where there are no more rows than compute units, eight up to twice as many, four beyond
 // (k = 5, bfloat16 rows of 131072 columns with 16, 8 and 4 wavefronts: 200 rows 16.2, 20.6 and 29.6 us, 400 30.2, 26.0 and 32.7, 700 44.8, 41.8 and
 // 38.2; without alternatives 200 12.8, 13.7 and 19.9, 400 23.5, 21.9 and 22.7, 700 35.8, 35.1 and 32.3).
 inline LogitsLayout logits_layout_whole(int64_t N, int M, int k) {
-  return {M <= 2048 && k <= 32 ? 1 : (N <= 256 ? 16 : (N <= 512 ? 8 : 4)), 1, M};
+  return {short_rows(N, M, k) ? 1 : (N <= 256 ? 16 : (N <= 512 ? 8 : 4)), 1, M};
 }
 
 inline LogitsLayout logits_layout(int64_t N, int M, int dtype, int k) {
@@ -67,11 +71,13 @@ inline HeldLayout held_layout(int M, int dtype) {
 }
 
 // The segments of a gradient whose row sums are known: 16 KiB (4096 x 131072 bfloat16: 340 us; 8 KiB 395, 32 KiB 350), less, down to 4 KiB, where
-// that leaves compute units without work.  A gradient that takes its logits' place has one: a row whose log-sum-exp is large is
-// read whole before any of it is written.
+// that leaves compute units without work; short rows of 16 bits take one wavefront (16384 x 1000 bfloat16 35 -> 26 us, lists of 32 41 -> 28; the
+// same in fp32 33 against 37).  A gradient that takes its logits' place has one segment: a row whose log-sum-exp is large is read whole before any of it
+// is written.
 inline LogitsLayout logits_grad_layout(int64_t N, int M, int dtype, bool in_place) {
-  if (in_place) return {4, 1, M};
   const int v = logits_width(dtype);
+  if (dtype != 0 && M <= 2048) return {1, 1, M};
+  if (in_place) return {4, 1, M};
   int64_t cols = 16384 / (dtype == 0 ? 4 : 2);
   while (cols > 1024 * v / 4 && N * ceil_div(M, cols) < 1024) cols /= 2;
   LogitsLayout l;

@@ -143,3 +143,21 @@ def test_eight_wavefronts_to_a_row(mask, dtype):
         got = R.rtopk_token_logprobs(x, t, k)
         check_forward(R, x[:9], xh[:9], t[:9], k, got=[g[:9] for g in got])
         check_forward(R, x[-9:], xh[-9:], t[-9:], k, got=[g[-9:] for g in got])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("mask", ["none", "few columns left", "none left", "all equal", "four levels", "ascending", "the type's lowest value", "a plateau at the end"])
+def test_one_wavefront_to_a_row(mask, dtype):
+    R = _gpu()
+    for N, M, k in ((4096, 2049, 32), (4100, 4999, 20), (4097, 700, 5), (4096, 16384, 1)):
+        x, xh = rows(N, M, dtype, seed=N + M, mask=MASKS.get(mask))
+        t = some_tokens(N, M, 1, k)
+        got = R.rtopk_token_logprobs(x, t, k)
+        check_forward(R, x[:9], xh[:9], t[:9], k, got=[g[:9] for g in got])
+        check_forward(R, x[-9:], xh[-9:], t[-9:], k, got=[g[-9:] for g in got])
+        lists = teacher_list(9, M, 20, 3)
+        loss, _ = R.rtopk_distill(x, lists[0].repeat(N // 9 + 1, 1)[:N].contiguous(), lists[1].repeat(N // 9 + 1, 1)[:N].contiguous())
+        want, _ = R.rtopk_distill(x[:9], *lists[:2])  # (another layout, checked elsewhere)
+        finite = torch.isfinite(want)
+        assert torch.equal(finite, torch.isfinite(loss[:9]))
+        torch.testing.assert_close(loss[:9][finite], want[finite], rtol=1e-5, atol=1e-5)
