@@ -1308,6 +1308,7 @@ __global__ __launch_bounds__(64 * W) void distill_row_kernel(LogitsArgs a) {
     const float loss = list_loss<DT>(a, row, t, base.less, list);
     if (threadIdx.x == 0) a.loss[n] = loss;
   }
+  __syncthreads();  // the first wavefront has read the logits that the loss needs: a gradient of zero may take their place at once
   const float up = a.inv_t * a.grad[n];
   base.alpha = up * head.mass;
   const bool empty = t.s == 0.0f;
