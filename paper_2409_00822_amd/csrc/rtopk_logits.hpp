@@ -679,8 +679,13 @@ __device__ Running stats_and_top(const Segment<DT>& g, int first, int k, float c
   } else if (all < k) {  // all finite ones are listed: those that are not follow in the first list
     __syncthreads();
     if (threadIdx.x < 64) {
-      const int filled = fill_list<DT, W>(g, first, k - all + n, kLowKey, n, room);
+      const int filled = fill_list<DT, W>(g, first, k - all + n, kLowKey, n, room), most = min(k, g.lead + g.full * L::V + g.rest);
       if (threadIdx.x == 0) room.listed[0] = filled;
+      // Fewer still: a signalling NaN, for which a maximum is NaN, hid columns beside it.  Nothing of such a row is a number: its first columns.
+      if (all - n + filled < most) {
+        for (int j = threadIdx.x; j < most; j += 64) room.found[j] = place_key(kLowKey, first + j);
+        set_listed(room, most);
+      }
     }
     __syncthreads();
   }
