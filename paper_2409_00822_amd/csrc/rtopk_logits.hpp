@@ -1011,7 +1011,8 @@ struct Base {
     float lq = __builtin_fmaf(x - m, inv_t, -less);
     if (ENT) lq = lq < kFar ? kFar : lq;  // (NaN stays)
     const float q = __builtin_amdgcn_exp2f(lq * kLog2e);
-    return ENT ? q * (alpha - beta * (lq + h)) : alpha * q;
+    // (q first: beta is 1 / T times a gradient and may be so large that beta ln q leaves fp32, where q is 0 above all)
+    return ENT ? __builtin_fmaf(-beta, q * (lq + h), alpha * q) : alpha * q;
   }
 };
 
