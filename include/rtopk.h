@@ -235,8 +235,9 @@ int rtopk_token_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t M
 /*
  * Gradient of the above with respect to the logits,
  *   (1 / T) (sum_g grad_logprobs_g (1[v == token_g] - q_v) - grad_entropy q_v (ln q_v + entropy)),
- * one launch; logits read once, gradient written once.  Rows whose tokens' gradients sum to zero (tokens left out have none) and whose entropy
- * has no gradient are not read.
+ * one launch; logits read once, gradient written once.  Where |lse| is above 1024 it has too few digits, and the row's sums are taken again: its logits are
+ * read twice where rows are many (up to five times where they are short), by several workgroups at once where they are few.  Rows whose tokens' gradients sum
+ * to zero (tokens left out have none) and whose entropy has no gradient are not read.
  *   grad_logprobs : [N][G] fp32 (NULL where G is 0).      grad_entropy : [N] fp32, or NULL: the entropy has no gradient.
  *   lse           : [N] fp32 as the forward call wrote it at the same temperature.   entropy : [N] fp32 likewise (with grad_entropy only).
  *   grad_logits   : [N][M] of `dtype`, rows grad_stride >= M apart.  It may be the logits themselves (same address and stride), which it then

@@ -1106,8 +1106,8 @@ __device__ __forceinline__ void write_gradient(const LogitsArgs& a, const ListRo
 
 // Bound by HBM: logits read once, gradient written once (4096 x 131072 bfloat16, an eighth of the rows not read, 339 us, 5.95 TB/s; 2048 x 65536 fp32,
 // lists of 100, 172 us, 6.24 TB/s; this repository's copy kernels reach 6.2 to 6.5).
-// A segment of a row's gradient by one workgroup.  The row's sums are known: its log-sum-exp was saved (JOIN false), or the segments' sums
-// lie in scratch memory (JOIN, distillation only), and then the loss is written too.
+// A segment of a row's gradient by one workgroup (several, where the row's sums are taken again).  The row's sums are known: its log-sum-exp was saved
+// (JOIN false), or the segments' sums lie in scratch memory (JOIN, distillation only), and then the loss is written too.
 template <int DT, int OP, bool ENT, bool JOIN, int W>
 __global__ __launch_bounds__(64 * W) void logits_grad_kernel(LogitsArgs a) {
   using L = Logits<DT>;
@@ -1120,17 +1120,19 @@ __global__ __launch_bounds__(64 * W) void logits_grad_kernel(LogitsArgs a) {
   const int64_t n = a.row0 + blockIdx.x / (uint32_t)a.segments;
   const auto* row = static_cast<const typename L::elem*>(a.x) + n * a.stride;
   auto* out = static_cast<typename L::elem*>(a.grad_x) + n * a.grad_stride;
-  const int first = seg * a.seg_cols, cols = min(a.seg_cols, a.M - first);
-  const Segment<DT> g(row + first, cols);
+  int first = seg * a.seg_cols, cols = min(a.seg_cols, a.M - first);
   if (threadIdx.x < 64) {
     if (OP == kOpTokens) token_list(a, n, list);
     else teacher_list(a, n, list);
   }
   Base base;
   base.inv_t = a.inv_t;
+  base.m = 0.0f;
+  base.less = JOIN ? 0.0f : a.lse_in[n];
+  const float up = OP == kOpTokens ? a.inv_t : a.inv_t * a.grad[n];
   bool empty;
+  __syncthreads();
   if constexpr (JOIN) {
-    __syncthreads();
     const Stats t = join_segments<false>(a, n, a.c);
     base.m = t.m;
     base.less = logf(t.s);
@@ -1140,22 +1142,25 @@ __global__ __launch_bounds__(64 * W) void logits_grad_kernel(LogitsArgs a) {
       if (threadIdx.x == 0) a.loss[n] = loss;
     }
   } else {
-    base.m = 0.0f;
-    base.less = a.lse_in[n];
     empty = base.less == kNegInf;
-    __syncthreads();
-    if (fabsf(base.less) > kLargeLse && fabsf(base.less) < __builtin_inff()) {
+    // (a row without a gradient is not read)
+    if (fabsf(base.less) > kLargeLse && fabsf(base.less) < __builtin_inff() && __any(up * head.mass != 0.0f || (ENT && a.inv_t * a.grad_entropy[n] != 0.0f))) {
+      // One of `far_group` workgroups takes the row's sums and writes the segments of all: another one in each row, for neighbours lie in different XCDs.
+      const int group = seg - seg % a.far_group, of = min(a.far_group, a.segments - group);
+      if (seg - group != (int)(n % of)) return;
+      first = group * a.seg_cols;
+      cols = min(of * a.seg_cols, a.M - first);
       const Segment<DT> all(row, a.M);
       const Stats t = segment_stats<DT, W, false>(all, thread_stats<DT, T, 4, false, true>(all, a.c), a.c, sums);
       base.m = t.m;
       base.less = logf(t.s);
     }
   }
-  const float up = OP == kOpTokens ? a.inv_t : a.inv_t * a.grad[n];
   base.alpha = OP == kOpTokens ? -up * head.mass : up * head.mass;
   base.beta = ENT ? a.inv_t * a.grad_entropy[n] : 0.0f;
   base.h = ENT ? a.entropy_in[n] : 0.0f;
   const bool zero = empty || (base.alpha == 0.0f && base.beta == 0.0f);
+  const Segment<DT> g(row + first, cols);
   write_gradient<DT, T, ENT>(a, list, g, first, cols, out + first, base, empty ? 0.0f : (OP == kOpTokens ? up : -up), zero);
 }
 

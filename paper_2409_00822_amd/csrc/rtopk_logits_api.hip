@@ -94,6 +94,7 @@ int backward(LogitsArgs& a, int dtype, int op, void* stream) {
   const rtopk::LogitsLayout l = rtopk::logits_grad_layout(a.N, a.M, dtype, in_place(a));
   a.segments = l.segments;
   a.seg_cols = l.cols;
+  a.far_group = rtopk::far_group(a.N, l.segments);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t err = sliced(a, [&](int64_t rows) { return rtopk::launch_logits_grad(dtype, op, l.waves, false, a, rows, s); });
   return err == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;

@@ -31,6 +31,7 @@ struct LogitsArgs {
   void* grad_x;
   int64_t grad_stride;
   int segments, seg_cols;
+  int far_group;  // (backward) segments that share a workgroup where the row's sums are taken again
   float4* part;         // [N][segments] maximum, S, A
   uint64_t* part_keys;  // [N][segments][k]
 };

@@ -88,6 +88,17 @@ inline LogitsLayout logits_grad_layout(int64_t N, int M, int dtype, bool in_plac
   return l;
 }
 
+// Where a saved log-sum-exp is so large that a row's sums are taken again, which the kernel finds out, this many segments of the row share a
+// workgroup, so that no more than about 512 workgroups, or one to a row, read a row whole (fp32 at T = 0.01, each segment's workgroup against this: 2048 x 65536 697 -> 316 us,
+// 16 x 1048576 728 -> 185, 512 x 32000 88 -> 53, 64 x 32000 14.9 -> 12.7; with 256 workgroups 128 x 32000 16.0 against 16.7, 256 x 32000 32.4
+// against 30.1).  Up to four segments read the row each, from the caches (1024 x 32000 bfloat16 54.7 against 61.7, 2048 x 8192 31.2 against 35.8).
+constexpr int kFarWorkgroups = 512;
+inline int far_group(int64_t N, int segments) {
+  if (segments <= 4) return 1;
+  const int64_t group = ceil_div(N * segments, kFarWorkgroups);
+  return group < segments ? (int)group : segments;
+}
+
 // Device memory for the segments' partial results: maximum, sum and weighted sum of each, then its alternatives.
 inline int64_t logits_workspace(int64_t N, const LogitsLayout& l, int k) {
   return l.segments > 1 ? N * l.segments * (16 + 8 * (int64_t)k) : 0;
