@@ -40,3 +40,32 @@ def test_workgroups_that_take_a_rows_sums_again(tmp_path):
     """Their number does not grow with the row's width once rows fill the GPU: what is read again is at most 4 times the rows, or 512 rows."""
     bad, grouped = run(tmp_path, FAR)
     assert bad == 0 and grouped > 0
+
+
+KERNELS = r"""
+int main() {
+  // rows by one workgroup at 97 rows, and the (wavefronts, loads) that hold them; columns of fp32, twice as many in 16 bits
+  const int columns[] = {256, 257, 1024, 4096, 4097, 8192, 8193, 16384, 16385, 32768, 32769, 49152, 49157, 65536, 65541};
+  for (int dtype = 0; dtype < 3; dtype += 2)
+    for (int M : columns) {
+      M = dtype == 0 ? M : 2 * M;
+      const HeldLayout h = held_layout(M, dtype);
+      printf("%d %d %d\n", logits_layout(97, M, dtype, 0).segments, h.waves, h.loads);
+    }
+  // the lines of the spread rows: segments with scratch memory
+  const int64_t calls[][4] = {{2, 32768, 0, 0}, {2, 32769, 0, 0}, {95, 32769, 0, 32}, {95, 32769, 0, 33}, {96, 32769, 0, 0}, {2, 65537, 2, 32}, {2, 65536, 2, 32}, {3, 262144, 0, 20}, {1, 1 << 20, 1, 9}};
+  for (const auto& c : calls) printf("%d\n", logits_layout(c[0], (int)c[1], (int)c[2], (int)c[3]).segments);
+  return 0;
+}
+"""
+
+
+def test_which_kernel_takes_a_row(tmp_path):
+    """The widths of the GPU tests reach the kernels that they are meant for."""
+    n = run(tmp_path, KERNELS)
+    rows = [tuple(n[3 * i:3 * i + 3]) for i in range(30)]
+    narrow = [(1, 1, 4)] * 3 + [(1, 4, 4)] * 2 + [(1, 4, 8)] * 2 + [(1, 8, 8)] * 2 + [(1, 8, 16)] * 2 + [(1, 8, 24)]
+    read_twice = (1, 8, 0)
+    assert rows[:15] == narrow + [(1, 16, 16)] * 2 + [read_twice]
+    assert rows[15:] == narrow + [(1, 8, 32)] * 2 + [read_twice]
+    assert n[90:] == [1, 9, 9, 1, 1, 9, 1, 64, 128]
