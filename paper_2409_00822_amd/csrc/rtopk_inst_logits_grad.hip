@@ -25,8 +25,9 @@ hipError_t grad_of_type(int op, int waves, bool join, const LogitsArgs& a, int64
 template <int DT>
 hipError_t row_of_type(int waves, int loads, const LogitsArgs& a, int64_t rows, hipStream_t s) {
   const dim3 grid((uint32_t)rows), block((uint32_t)(64 * waves));
-#define X(w, r, q) \
-  if (waves == w && loads == r + q) return launch_kernel(distill_held_kernel<DT, w, r, q>, grid, block, list_bytes(a.k), s, a);
+#define X(w, r, q)                     \
+  if constexpr (is_held_by(DT, w, r)) \
+    if (waves == w && loads == r + q) return launch_kernel(distill_held_kernel<DT, w, r, q>, grid, block, list_bytes(a.k), s, a);
   RTOPK_HELD_LIST(X)
 #undef X
   return launch_kernel(distill_row_kernel<DT, 8>, grid, dim3(512), list_bytes(a.k), s, a);

@@ -69,3 +69,30 @@ def test_which_kernel_takes_a_row(tmp_path):
     assert rows[:15] == narrow + [(1, 16, 16)] * 2 + [read_twice]
     assert rows[15:] == narrow + [(1, 8, 32)] * 2 + [read_twice]
     assert n[90:] == [1, 9, 9, 1, 1, 9, 1, 64, 128]
+
+
+REACHED = r"""
+int main() {
+  // every kernel that is compiled for a type is some width's, and every width's is compiled
+  int bad = 0, kernels = 0;
+  for (int dtype = 0; dtype < 3; ++dtype) {
+#define X(w, r, q)                                            \
+  {                                                           \
+    bool found = false;                                       \
+    for (int M = 1; M <= 200000; ++M) {                       \
+      const HeldLayout h = held_layout(M, dtype);             \
+      found |= h.waves == w && h.loads == r + q;              \
+    }                                                         \
+    bad += found != is_held_by(dtype, w, r);                  \
+    kernels += found;                                         \
+  }
+    RTOPK_HELD_LIST(X)
+  }
+  printf("%d %d\n", bad, kernels);
+  return 0;
+}
+"""
+
+
+def test_every_kernel_that_holds_a_row_is_reached(tmp_path):
+    assert run(tmp_path, REACHED) == [0, 21]
