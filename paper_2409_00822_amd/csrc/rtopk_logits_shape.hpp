@@ -35,8 +35,11 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // against 11.2; 64 x 32000 fp32, k = 20, 13.4 against 10.0.
 inline bool spread(int64_t N, int64_t row_bytes, int k) { return N < 96 && row_bytes > 131072 && k <= 32; }
 
-// Rows that one wavefront takes: up to 2048 columns, and up to 16384 where there are rows enough to fill the GPU so, which pays no barriers (16384 x 4000
-// bfloat16 36 -> 25 us, with 5 alternatives 62 -> 39; 8192 x 16000, 5 alternatives 64 -> 56; 1000 x 4000, 5 alternatives 8.1 against 9.4).
+// Rows that one wavefront takes: up to 2048 columns, and up to 16384 where there are rows enough to fill the GPU so, which pays no barriers.
+// Four wavefronts and one, us: 16384 x 2500 bfloat16 30.2 and 17.8, with 5 alternatives 62.5 and 32.8, distillation 33.5 and 23.0; 16384 x 4000
+// 31.5 and 24.3, 58.6 and 37.9, 32.1 and 27.1; 4096 x 16000 24.2 and 24.3, 33.6 and 29.6, 24.6 and 23.2.  fp32 with alternatives likewise (16384 x 4000, 5
+// alternatives 53.6 and 48.2); without them it gains and loses (16384 x 4000 39.1 and 40.9, distillation 43.2 and 46.9; 4096 x 8000 22.9 and 22.1, 23.7 and
+// 21.8; 4096 x 16000 41.3 and 41.4, 42.7 and 41.6).  Fewer rows lose: 1000 x 4000 bfloat16, 5 alternatives 8.1 and 9.4.
 inline bool short_rows(int64_t N, int M, int k) { return k <= 32 && (M <= 2048 || (M <= 16384 && N >= 4096)); }
 
 // A workgroup for each row: one wavefront for short rows; sixteen where there are no more rows than compute units, eight up to twice as many, four beyond
