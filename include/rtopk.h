@@ -53,13 +53,13 @@ enum {
   RTOPK_ERR_NULL_POINTER = -1,  /* a data pointer is NULL while N > 0 */
   RTOPK_ERR_BAD_SHAPE = -2,     /* N < 0, M < 1, k < 1 or k > M */
   RTOPK_ERR_BAD_MAX_ITER = -3,  /* max_iter < 0 */
-  RTOPK_ERR_M_TOO_LARGE = -4,   /* M > rtopk_max_m(); M > 65536 for 16-bit rows, dense form, backward edge; M > 256 for *_u8 */
+  RTOPK_ERR_M_TOO_LARGE = -4,   /* M > rtopk_max_m(); M > 65536 for 16-bit rows, dense form, backward edge; M > 256 for *_u8; more than 1024 experts */
   RTOPK_ERR_MISALIGNED = -5,    /* a pointer is not aligned to its element size */
   RTOPK_ERR_LAUNCH = -6,        /* the HIP runtime refused the launch */
   RTOPK_ERR_BAD_EPSILON = -7,   /* eps_rel is negative or NaN */
   RTOPK_ERR_OVERLAP = -8,       /* the input shares bytes with an output, or two outputs with each other */
-  RTOPK_ERR_BAD_TEMPERATURE = -9, /* a temperature that is not positive and finite, or whose reciprocal is not */
-  RTOPK_ERR_BAD_TYPE = -10      /* an element type that is none of RTOPK_F32, RTOPK_F16, RTOPK_BF16, or token_bytes neither 4 nor 8 */
+  RTOPK_ERR_BAD_TEMPERATURE = -9, /* a temperature that is not positive and finite, or whose reciprocal is not (0 is one where tokens are drawn) */
+  RTOPK_ERR_BAD_TYPE = -10      /* an element type that is none of RTOPK_F32, RTOPK_F16, RTOPK_BF16, token_bytes neither 4 nor 8, or col_bytes neither 1 nor 4 */
 };
 
 /*
@@ -277,6 +277,78 @@ int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dt
                             const void* teacher_vals, int32_t teacher_dtype, const int32_t* teacher_cols, int32_t k, int32_t log_probs,
                             float temperature, float* out_loss, void* grad_logits, int64_t grad_stride, void* workspace,
                             int64_t workspace_bytes, void* stream);
+
+/*
+ * Tokens drawn from rows of logits, and drafted tokens verified
+ * --------------------------------------------------------------
+ * Random numbers are inputs, and a result is a pure function of its inputs: differences, powers and sums are 64-bit, taken in an order that
+ * depends on the call's sizes only.  A row x at temperature T has probabilities p_v = exp((x_v - max x) / T) / sum; at T = 0 all of it is on the largest logit, the
+ * lowest column of equal ones.  By a number u in [0, 1) it gives the lowest column v with  p_0 + ... + p_v > u  (u below 0 or NaN counts as 0; where rounding or
+ * u >= 1 leaves none, the last column with p_v > 0).  A row without a distribution -- nothing but -inf, or with a NaN, or with +inf at T > 0 -- gives -1.
+ *
+ *   logits       : as above; rows may lie apart by any stride >= M.
+ *   uniforms     : fp32 (NULL where `temperature` is 0 and temperatures is NULL).
+ *   temperatures : [N] or [B] fp32 on the device, one for each sequence, or NULL: `temperature` for all.  0 is the limit above; a sequence whose
+ *                  temperature is negative, infinite or NaN gets no token (-1) and no draft accepted.
+ *   temperature  : 0, or finite and positive with a finite reciprocal (RTOPK_ERR_BAD_TEMPERATURE); not looked at where temperatures is given.
+ *   token_bytes  : of drafts and out_tokens, 4 (int32_t) or 8 (int64_t).
+ *   workspace    : as above, rtopk_verify_workspace_bytes(...) bytes (for rtopk_sample_tokens with G and draft_logits 0): few sequences are then spread
+ *                  over many workgroups, in a few launches.  Drawn tokens of both ways can differ only where u lies within rounding, about 1e-13, of a border.
+ */
+int64_t rtopk_verify_workspace_bytes(int64_t B, int32_t G, int32_t M, int32_t dtype, int32_t draft_logits);
+
+/* One token of each row: out_tokens [N], by uniforms [N]. */
+int rtopk_sample_tokens(const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride, const float* uniforms, const float* temperatures,
+                        double temperature, void* out_tokens, int32_t token_bytes, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens: a sequence's drafts d_0, d_1, ... are accepted from the first on while  u_i q_i(d_i) < p_i(d_i),  p_i and q_i the
+ * distributions of row i of the target and of the draft model.  The first rejected one, at n, is replaced by a draw by u_G from max(p_n - q_n, 0) (from p_n where
+ * that sums to no more than 2^-40); where all are accepted one more token is drawn by u_G from the row behind them.  The tokens are then distributed
+ * as if drawn from the target one by one, if the drafts were drawn from q.
+ *   target_logits : [B][G + 1][M], sequences target_seq_stride and their rows target_pos_stride elements apart, each >= M, in any order.
+ *   draft_logits  : [B][G][M] of the same type, likewise; NULL: a draft stands for itself, q_i(d_i) = 1 (as where T is 0).  A row of nothing but -inf has q = 0.
+ *   drafts        : [B][G], 0 <= G <= 128.  The first token outside [0, M) ends a sequence's drafts; rows behind the one that the last token is drawn from are not
+ *                   looked at.
+ *   uniforms      : [B][G + 1].
+ *   out_tokens    : [B][G + 1]: the accepted drafts, the drawn token, -1 behind it.     out_accepted : [B] int32_t, how many were accepted (optional).
+ */
+int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype, int64_t B, int32_t G, int32_t M, int64_t target_seq_stride,
+                        int64_t target_pos_stride, int64_t draft_seq_stride, int64_t draft_pos_stride, const void* drafts, int32_t token_bytes,
+                        const float* uniforms, const float* temperatures, double temperature, void* out_tokens, int32_t* out_accepted, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/*
+ * A router's balance loss
+ * -----------------------
+ * N tokens in `groups` groups of N / groups consecutive ones (sequences, or 1: the whole batch); a token has E logits x and the k columns that a selection
+ * (rtopk_rowwise*) picked for it.  A column outside [0, E) is no pick, and a token without any (padding) is left out of everything.  With p = softmax(x), n the
+ * group's tokens that count, counts_e its picks of expert e, f_e = counts_e / sum counts, P_e = (1 / n) sum_t p_te:
+ *   loss = E sum_e f_e P_e  (1 where picks or probabilities are even; 0 for a group without picks),      z = (1 / n) sum_t lse_t^2.
+ * Sums over tokens are 64-bit, over at most 64 terms fp32.  A row of nothing but -inf has probabilities 0 and adds nothing to z; a NaN or +inf spoils
+ * its group's results, and no other's.
+ *   logits     : [N][E] of `dtype`, rows `stride` >= E elements apart, 1 <= E <= 1024 (RTOPK_ERR_M_TOO_LARGE beyond).
+ *   cols       : [N][k], int32_t or uint8_t (col_bytes 4 or 1; bytes: E <= 256), 1 <= k <= E, in any order; the same column twice counts twice.
+ *   out_loss, out_z (optional) : [groups] fp32.     out_probs (optional) : [groups][E] fp32, P.     out_counts : [groups][E] int32_t.
+ *   out_rows   : [groups] int32_t, n.
+ *   workspace  : as above, rtopk_balance_workspace_bytes(...) bytes.
+ */
+int64_t rtopk_balance_workspace_bytes(int64_t N, int32_t E, int32_t dtype, int32_t groups);
+int rtopk_balance_loss(const void* logits, int32_t dtype, int64_t N, int32_t E, int64_t stride, const void* cols, int32_t col_bytes, int32_t k,
+                       int32_t groups, float* out_loss, float* out_z, float* out_probs, int32_t* out_counts, int32_t* out_rows, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of sum_g (grad_loss_g loss_g + grad_z_g z_g) + sum grad_vals . (the picked logits) with respect to the logits; the counts are constants.
+ *   grad_loss  : [groups] fp32.     grad_z : [groups] fp32, or NULL.     grad_vals : [N][k] fp32, gradients of the picked values (as rtopk_maxk_backward
+ *                takes them), or NULL; those of the same column add up.
+ *   counts, rows : as rtopk_balance_loss wrote them (counts may be sums over several processes, whose shares then are the whole's).
+ *   grad_logits  : [N][E] of `dtype`, rows grad_stride >= E apart, rounded once; zero for tokens left out.  It may be the logits themselves (same address and
+ *                  stride); any other overlap is RTOPK_ERR_OVERLAP.
+ */
+int rtopk_balance_loss_backward(const float* grad_loss, const float* grad_z, const float* grad_vals, const void* logits, int32_t dtype, int64_t N, int32_t E,
+                                int64_t stride, const void* cols, int32_t col_bytes, int32_t k, int32_t groups, const int32_t* counts, const int32_t* rows,
+                                void* grad_logits, int64_t grad_stride, void* stream);
 
 /* Human-readable text for a status code (static storage, never NULL). */
 const char* rtopk_status_string(int status);

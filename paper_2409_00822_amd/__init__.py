@@ -1,10 +1,21 @@
-"""MI355X-native row-wise top-k selection (RTop-K, arXiv 2409.00822) and operators on rows of logits: thin Python binding over the
+"""MI355X-native row-wise top-k selection (RTop-K, arXiv 2409.00822), operators on rows of logits, drawn and
+verified tokens, and a router's balance loss: thin Python binding over the
 C-ABI library `librtopk.so` (hand-written HIP kernels for gfx950).
 
 The binding only marshals arguments: device pointers of torch tensors and the current HIP stream go
 straight to the C entry points declared in include/rtopk.h.  There is no CPU fallback; if the
 library is missing the import of `rtopk` functions fails loudly.
 """
+from .balance import (  # noqa: F401
+    rtopk_balance_loss,
+    rtopk_balance_loss_backward,
+    rtopk_balance_workspace_bytes,
+)
+from .draw import (  # noqa: F401
+    rtopk_sample_tokens,
+    rtopk_verify_drafts,
+    rtopk_verify_workspace_bytes,
+)
 from .logits import (  # noqa: F401
     rtopk_distill,
     rtopk_distill_backward,

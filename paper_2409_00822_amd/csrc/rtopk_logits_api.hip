@@ -5,35 +5,14 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "rtopk_checks.hpp"
 #include "rtopk_dispatch.hpp"
 #include "rtopk_logits_dispatch.hpp"
 
 namespace {
 
+using namespace rtopk::checks;
 using rtopk::LogitsArgs;
-
-inline uintptr_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
-
-struct Buffer {
-  const void* p;
-  uint64_t bytes, align;
-  bool written;
-};
-
-// RTOPK_OK, or what is wrong with the buffers: alignment, or bytes that a written one shares with another.
-template <int C>
-int check_buffers(const Buffer (&b)[C]) {
-  for (const Buffer& x : b)
-    if (!rtopk::is_aligned(addr(x.p), x.align)) return RTOPK_ERR_MISALIGNED;
-  for (int i = 0; i < C; ++i)
-    for (int j = i + 1; j < C; ++j)
-      if ((b[i].written || b[j].written) && b[i].p && b[j].p && rtopk::ranges_overlap(addr(b[i].p), b[i].bytes, addr(b[j].p), b[j].bytes))
-        return RTOPK_ERR_OVERLAP;
-  return RTOPK_OK;
-}
-
-inline uint64_t size_of(int dtype) { return dtype == RTOPK_F32 ? 4 : 2; }
-inline bool is_type(int dtype) { return dtype == RTOPK_F32 || dtype == RTOPK_F16 || dtype == RTOPK_BF16; }
 
 // The part of the checks that all share, and the arguments they fill.
 int rows_of_logits(LogitsArgs& a, const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride, float temperature) {

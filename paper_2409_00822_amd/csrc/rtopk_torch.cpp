@@ -13,8 +13,10 @@
 #include <ATen/ops/empty.h>
 #include <ATen/record_function.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 
+#include <cstdint>
 #include <exception>
 #include <limits>
 
@@ -555,6 +557,207 @@ PyObject* distill_with_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// Scratch memory of n bytes, if there is any.
+struct Memory {
+  Tensor tensor;
+  void* data = nullptr;
+  int64_t bytes = 0;
+  Memory(int64_t n, c10::Device device, bool plain) {
+    if (n <= 0) return;
+    try {
+      tensor = new_tensor({n}, at::kByte, device, plain);
+      data = tensor.data_ptr();
+      bytes = n;
+    } catch (const c10::OutOfMemoryError&) {
+    }
+  }
+};
+
+// Random numbers and temperatures: a number for all, or a tensor with one for each.
+struct Random {
+  const float *uniforms = nullptr, *temperatures = nullptr;
+  double temperature = 1.0;
+  bool set(PyObject* u, PyObject* t, at::IntArrayRef shape, int64_t B, c10::Device device) {
+    if (const Tensor* per = tensor_of(t)) {
+      if (!is_vector(per, at::kFloat, B, device)) return false;
+      temperatures = static_cast<const float*>(per->data_ptr());
+    } else {
+      if (!PyFloat_Check(t) && !PyLong_Check(t)) return false;
+      temperature = PyFloat_AsDouble(t);
+      if (temperature == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+      }
+    }
+    if (u == Py_None) return !temperatures && temperature == 0.0;
+    const Tensor* x = tensor_of(u);
+    if (!x || x->device() != device || x->scalar_type() != at::kFloat || !x->is_contiguous() || x->sizes() != shape) return false;
+    uniforms = static_cast<const float*>(x->data_ptr());
+    return true;
+  }
+};
+
+// sample_tokens(logits, uniforms, temperature, out_tokens)
+PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const Tensor* x = n == 4 ? tensor_of(args[0]) : nullptr;
+    Rows r;
+    Random u;
+    if (!r.set(x) || !u.set(args[1], args[2], {r.N}, r.N, x->device())) return none();
+    const Tensor* given = tensor_of(args[3]);
+    const at::ScalarType type = given && given->scalar_type() == at::kInt ? at::kInt : at::kLong;
+    const bool plain = is_plain();
+    Output out;
+    if (!out.set(args[3], type, {r.N}, x->device(), plain) || out.tensor.device() != x->device()) return failed();
+    void* p = out.tensor.data_ptr();
+    void* s = stream_of(*x);
+    Memory w(rtopk_verify_workspace_bytes(r.N, 0, r.M, r.dtype, 0), x->device(), plain);
+    const c10::hip::HIPGuard on(x->device().index());
+    const int status = unlocked([&] {
+      return rtopk_sample_tokens(r.data, r.dtype, r.N, r.M, r.stride, u.uniforms, u.temperatures, u.temperature, p, type == at::kInt ? 4 : 8, w.data,
+                                 w.bytes, s);
+    });
+    return status == RTOPK_OK ? out.release() : none();
+  });
+}
+
+// Rows of logits of sequences, [B, positions, M].
+struct Sequences {
+  void* data = nullptr;
+  int64_t B = 0, P = 0, seq = 0, pos = 0;
+  int32_t M = 0, dtype = 0;
+  bool set(const Tensor* t) {
+    if (!t || !t->is_cuda() || t->dim() != 3 || t->size(2) > std::numeric_limits<int32_t>::max()) return false;
+    const at::ScalarType type = t->scalar_type();
+    if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return false;
+    dtype = type == at::kFloat ? RTOPK_F32 : (type == at::kHalf ? RTOPK_F16 : RTOPK_BF16);
+    B = t->size(0);
+    P = t->size(1);
+    M = (int32_t)t->size(2);
+    seq = B > 1 ? t->stride(0) : M;
+    pos = P > 1 ? t->stride(1) : M;
+    data = t->data_ptr();
+    return (t->stride(2) == 1 || M <= 1) && seq >= M && pos >= M;
+  }
+};
+
+// verify_drafts(target_logits, drafts, uniforms, draft_logits, temperature, out_tokens, out_accepted)
+PyObject* verify_drafts(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const Tensor* x = n == 7 ? tensor_of(args[0]) : nullptr;
+    const Tensor* d = x ? tensor_of(args[1]) : nullptr;
+    Sequences t, q;
+    Random u;
+    if (!t.set(x) || t.P < 1 || t.P > 1024 || !d || d->device() != x->device() || !d->is_contiguous() || d->dim() != 2 || d->size(0) != t.B ||
+        d->size(1) != t.P - 1 || (d->scalar_type() != at::kInt && d->scalar_type() != at::kLong))
+      return none();
+    if (!u.set(args[2], args[4], {t.B, t.P}, t.B, x->device())) return none();
+    if (args[3] != Py_None) {
+      const Tensor* y = tensor_of(args[3]);
+      if (!q.set(y) || y->device() != x->device() || q.dtype != t.dtype || q.B != t.B || q.P != t.P - 1 || q.M != t.M) return none();
+    }
+    const bool plain = is_plain();
+    Output out, accepted;
+    if (!out.set(args[5], d->scalar_type(), {t.B, t.P}, x->device(), plain) || out.tensor.device() != x->device() ||
+        !accepted.set(args[6], at::kInt, {t.B}, x->device(), plain) || accepted.tensor.device() != x->device())
+      return failed();
+    const void* p_d = d->data_ptr();
+    const int bytes = d->scalar_type() == at::kInt ? 4 : 8;
+    void* p_out = out.tensor.data_ptr();
+    int32_t* p_accepted = static_cast<int32_t*>(accepted.tensor.data_ptr());
+    void* s = stream_of(*x);
+    const int G = (int)(t.P - 1);
+    Memory w(rtopk_verify_workspace_bytes(t.B, G, t.M, t.dtype, q.data ? 1 : 0), x->device(), plain);
+    const c10::hip::HIPGuard on(x->device().index());
+    const int status = unlocked([&] {
+      return rtopk_verify_drafts(t.data, q.data, t.dtype, t.B, G, t.M, t.seq, t.pos, q.seq, q.pos, p_d, bytes, u.uniforms, u.temperatures, u.temperature,
+                                 p_out, p_accepted, w.data, w.bytes, s);
+    });
+    return status == RTOPK_OK ? tuple_of(out, accepted) : none();
+  });
+}
+
+// A router's picks: columns [N, k], 32 bits or bytes.
+struct Picks {
+  const void* data = nullptr;
+  int32_t bytes = 0, k = 0;
+  bool set(const Tensor* t, int64_t N, c10::Device device) {
+    if (!t || t->device() != device || !t->is_contiguous() || t->dim() != 2 || t->size(0) != N || t->size(1) > 1024) return false;
+    if (t->scalar_type() != at::kInt && t->scalar_type() != at::kByte) return false;
+    bytes = t->scalar_type() == at::kInt ? 4 : 1;
+    k = (int32_t)t->size(1);
+    data = t->data_ptr();
+    return true;
+  }
+};
+
+// balance_loss(logits, cols, groups, out_loss, out_z, out_probs, out_counts, out_rows)
+PyObject* balance_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    int32_t groups;
+    const Tensor* x = n == 8 ? tensor_of(args[0]) : nullptr;
+    Rows r;
+    Picks c;
+    if (!r.set(x) || !c.set(tensor_of(args[1]), r.N, x->device()) || !int32_of(args[2], groups) || groups < 1) return none();
+    const c10::Device device = x->device();
+    const bool plain = is_plain();
+    Output loss, z, probs, counts, rows;
+    if (!loss.set(args[3], at::kFloat, {groups}, device, plain) || !z.set(args[4], at::kFloat, {groups}, device, plain) ||
+        !probs.set(args[5], at::kFloat, {groups, r.M}, device, plain) || !counts.set(args[6], at::kInt, {groups, r.M}, device, plain) ||
+        !rows.set(args[7], at::kInt, {groups}, device, plain))
+      return failed();
+    for (const Output* o : {&loss, &z, &probs, &counts, &rows})
+      if (o->tensor.device() != device) return none();
+    float *p_loss = floats(loss), *p_z = floats(z), *p_probs = floats(probs);
+    int32_t *p_counts = static_cast<int32_t*>(counts.tensor.data_ptr()), *p_rows = static_cast<int32_t*>(rows.tensor.data_ptr());
+    void* s = stream_of(*x);
+    Memory w(rtopk_balance_workspace_bytes(r.N, r.M, r.dtype, groups), device, plain);
+    const c10::hip::HIPGuard on(device.index());
+    const int status = unlocked([&] {
+      return rtopk_balance_loss(r.data, r.dtype, r.N, r.M, r.stride, c.data, c.bytes, c.k, groups, p_loss, p_z, p_probs, p_counts, p_rows, w.data, w.bytes, s);
+    });
+    return status == RTOPK_OK ? tuple_of(loss, z, probs, counts, rows) : none();
+  });
+}
+
+// balance_loss_backward(grad_loss, logits, cols, counts, rows, grad_z, grad_vals, grad_logits)
+PyObject* balance_loss_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const Tensor* x = n == 8 ? tensor_of(args[1]) : nullptr;
+    const Tensor* counts = x ? tensor_of(args[3]) : nullptr;
+    Rows r;
+    Picks c;
+    if (!r.set(x) || !c.set(tensor_of(args[2]), r.N, x->device()) || !counts || counts->dim() != 2 || counts->size(0) < 1 || counts->size(0) > INT32_MAX) return none();
+    const c10::Device device = x->device();
+    const int32_t groups = (int32_t)counts->size(0);
+    const Tensor *g = tensor_of(args[0]), *rows = tensor_of(args[4]);
+    if (counts->device() != device || !is_shape(*counts, at::kInt, groups, r.M) || !is_vector(rows, at::kInt, groups, device) ||
+        !is_vector(g, at::kFloat, groups, device))
+      return none();
+    const float *p_g = static_cast<const float*>(g->data_ptr()), *p_z = nullptr, *p_v = nullptr;
+    if (args[5] != Py_None) {
+      const Tensor* z = tensor_of(args[5]);
+      if (!is_vector(z, at::kFloat, groups, device)) return none();
+      p_z = static_cast<const float*>(z->data_ptr());
+    }
+    if (args[6] != Py_None) {
+      const Tensor* v = tensor_of(args[6]);
+      if (!v || v->device() != device || !is_shape(*v, at::kFloat, r.N, c.k)) return none();
+      p_v = static_cast<const float*>(v->data_ptr());
+    }
+    Gradient d;
+    if (!d.set(args[7], *x, r, is_plain())) return failed();
+    const int32_t *p_counts = static_cast<const int32_t*>(counts->data_ptr()), *p_rows = static_cast<const int32_t*>(rows->data_ptr());
+    void* s = stream_of(*x);
+    const c10::hip::HIPGuard on(device.index());
+    const int status = unlocked([&] {
+      return rtopk_balance_loss_backward(p_g, p_z, p_v, r.data, r.dtype, r.N, r.M, r.stride, c.data, c.bytes, c.k, groups, p_counts, p_rows, d.rows.data,
+                                         d.rows.stride, s);
+    });
+    return status == RTOPK_OK ? d.made.release() : none();
+  });
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -566,7 +769,10 @@ PyMethodDef kMethods[] = {
     {"gather", fast(gather), METH_FASTCALL, nullptr},   {"token_logprobs", fast(token_logprobs), METH_FASTCALL, nullptr},
     {"token_logprobs_backward", fast(token_logprobs_backward), METH_FASTCALL, nullptr},
     {"distill", fast(distill), METH_FASTCALL, nullptr}, {"distill_backward", fast(distill_backward), METH_FASTCALL, nullptr},
-    {"distill_with_grad", fast(distill_with_grad), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
+    {"distill_with_grad", fast(distill_with_grad), METH_FASTCALL, nullptr},
+    {"sample_tokens", fast(sample_tokens), METH_FASTCALL, nullptr}, {"verify_drafts", fast(verify_drafts), METH_FASTCALL, nullptr},
+    {"balance_loss", fast(balance_loss), METH_FASTCALL, nullptr},
+    {"balance_loss_backward", fast(balance_loss_backward), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr},
 };
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_rtopk_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

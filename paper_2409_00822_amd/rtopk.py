@@ -70,8 +70,18 @@ def load_library() -> ctypes.CDLL:
         lib.rtopk_distill.argtypes = [*rows, *teacher, f32, vp, vp, vp, i64, vp]
         lib.rtopk_distill_backward.argtypes = [vp, *rows, *teacher, vp, f32, vp, i64, vp]
         lib.rtopk_distill_with_grad.argtypes = [vp, *rows, *teacher, f32, vp, vp, i64, vp, i64, vp]
+        lib.rtopk_verify_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+        lib.rtopk_verify_workspace_bytes.restype = i64
+        draw = [vp, vp, ctypes.c_double]  # uniforms, temperatures, temperature
+        lib.rtopk_sample_tokens.argtypes = [*rows, *draw, vp, i32, vp, i64, vp]
+        lib.rtopk_verify_drafts.argtypes = [vp, vp, i32, i64, i32, i32, i64, i64, i64, i64, vp, i32, *draw, vp, vp, vp, i64, vp]
+        lib.rtopk_balance_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        lib.rtopk_balance_workspace_bytes.restype = i64
+        picks = [vp, i32, i32, i32]  # cols, col_bytes, k, groups
+        lib.rtopk_balance_loss.argtypes = [*rows, *picks, vp, vp, vp, vp, vp, vp, i64, vp]
+        lib.rtopk_balance_loss_backward.argtypes = [vp, vp, vp, *rows, *picks, vp, vp, vp, i64, vp]
         for name in ("rtopk_token_logprobs", "rtopk_token_logprobs_backward", "rtopk_distill", "rtopk_distill_backward",
-                     "rtopk_distill_with_grad"):
+                     "rtopk_distill_with_grad", "rtopk_sample_tokens", "rtopk_verify_drafts", "rtopk_balance_loss", "rtopk_balance_loss_backward"):
             getattr(lib, name).restype = ctypes.c_int
         lib.rtopk_status_string.argtypes = [ctypes.c_int]
         lib.rtopk_status_string.restype = ctypes.c_char_p
