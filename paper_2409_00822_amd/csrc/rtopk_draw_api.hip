@@ -8,7 +8,6 @@
 #include "rtopk_checks.hpp"
 #include "rtopk_dispatch.hpp"
 #include "rtopk_draw_dispatch.hpp"
-#include "rtopk_logits_shape.hpp"
 
 namespace {
 
@@ -31,7 +30,8 @@ extern "C" {
 
 int64_t rtopk_verify_workspace_bytes(int64_t B, int32_t G, int32_t M, int32_t dtype, int32_t draft_logits) {
   if (B < 1 || G < 0 || G > rtopk::kMaxDrafts || M < 1 || M > rtopk::kMaxLogitsM || !is_type(dtype) || (draft_logits & ~1) != 0) return 0;
-  return 0;
+  const bool draft = draft_logits != 0 && G > 0;
+  return rtopk::draw_workspace(B, G, draft, rtopk::draw_layout(B, G, M, dtype, draft));
 }
 
 int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype, int64_t B, int32_t G, int32_t M, int64_t target_seq_stride,
@@ -80,10 +80,27 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
   a.tokens = out_tokens;
   a.accepted = out_accepted;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int64_t most = 1 << 21;  // workgroups of a launch
-  for (a.row0 = 0; a.row0 < B; a.row0 += most)
-    if (rtopk::launch_draw(dtype, a, B - a.row0 < most ? B - a.row0 : most, s) != hipSuccess) return RTOPK_ERR_LAUNCH;
-  return RTOPK_OK;
+  const bool draft = draft_logits != nullptr;
+  rtopk::DrawLayout l = rtopk::draw_layout(B, G, M, dtype, draft);
+  if (l.segments > 1 && (!workspace || workspace_bytes < rtopk::draw_workspace(B, G, draft, l))) l = rtopk::draw_layout_whole(B, M);
+  hipError_t err = hipSuccess;
+  // launch(sequences) for slices whose workgroups fit one launch (2^31 threads)
+  const auto sliced = [&](int64_t each, auto launch) {
+    const int64_t most = (1 << 21) / each;
+    for (a.row0 = 0; a.row0 < B && err == hipSuccess; a.row0 += most) err = launch(B - a.row0 < most ? B - a.row0 : most);
+  };
+  if (l.segments > 1) {
+    a.segments = l.segments;
+    a.seg_cols = l.cols;
+    a.part = static_cast<double2*>(workspace);
+    a.rest = reinterpret_cast<double*>(a.part + B * rtopk::draw_rows(G, draft) * l.segments);
+    a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.segments);
+    sliced((int64_t)rtopk::draw_rows(G, draft) * l.segments, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
+    sliced(l.segments, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
+  } else {
+    sliced(1, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
+  }
+  return err == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;
 }
 
 int rtopk_sample_tokens(const void* logits, int32_t dtype, int64_t N, int32_t M, int64_t stride, const float* uniforms, const float* temperatures,

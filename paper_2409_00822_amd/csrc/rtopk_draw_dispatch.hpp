@@ -4,9 +4,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-namespace rtopk {
+#include "rtopk_draw_shape.hpp"
 
-constexpr int kMaxDrafts = 128;  // drafted tokens of a sequence
+namespace rtopk {
 
 // A call's arguments; what it does not use is null or 0.
 struct DrawArgs {
@@ -22,8 +22,16 @@ struct DrawArgs {
   int64_t B, row0;  // sequences; first one of the launch
   void* tokens;     // [B][G + 1], as the drafts
   int32_t* accepted;  // [B], optional
+  // sequences spread over workgroups
+  int segments, seg_cols;
+  double2* part;     // [B][rows][segments] masses; rows: G + 1 of the target, G of the draft
+  double* rest;      // [B][segments] sums of max(p - q, 0)
+  int32_t* arrived;  // [B]
 };
 
-hipError_t launch_draw(int dtype, const DrawArgs& a, int64_t rows, hipStream_t stream);
+// Each enqueues its kernel for sequences [a.row0, a.row0 + n).
+hipError_t launch_draw(int dtype, int waves, const DrawArgs& a, int64_t n, hipStream_t stream);  // a workgroup to a sequence
+hipError_t launch_draw_mass(int dtype, const DrawArgs& a, int64_t n, hipStream_t stream);
+hipError_t launch_draw_join(int dtype, const DrawArgs& a, int64_t n, hipStream_t stream);
 
 }  // namespace rtopk

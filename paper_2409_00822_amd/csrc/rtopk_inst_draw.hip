@@ -6,14 +6,35 @@ namespace rtopk {
 namespace {
 
 template <int DT>
-hipError_t draw_of_type(const DrawArgs& a, int64_t rows, hipStream_t s) {
-  return launch_kernel(draw_kernel<DT, 16>, dim3((uint32_t)rows), dim3(1024), 0, s, a);
+hipError_t draw_of_type(int waves, const DrawArgs& a, int64_t n, hipStream_t s) {
+  const dim3 grid((uint32_t)n), block(64 * waves);
+  return waves == 4   ? launch_kernel(draw_kernel<DT, 4>, grid, block, 0, s, a)
+         : waves == 8 ? launch_kernel(draw_kernel<DT, 8>, grid, block, 0, s, a)
+                      : launch_kernel(draw_kernel<DT, 16>, grid, block, 0, s, a);
+}
+
+template <int DT>
+hipError_t mass_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
+  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * draw_rows(a.G, a.draft != nullptr) * a.segments)), dim3(256), 0, s, a);
+}
+
+template <int DT>
+hipError_t join_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
+  return launch_kernel(draw_join_kernel<DT>, dim3((uint32_t)(n * (a.draft ? a.segments : 1))), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
-hipError_t launch_draw(int dtype, const DrawArgs& a, int64_t rows, hipStream_t s) {
-  return dtype == kF32 ? draw_of_type<kF32>(a, rows, s) : dtype == kF16 ? draw_of_type<kF16>(a, rows, s) : draw_of_type<kBF16>(a, rows, s);
+hipError_t launch_draw(int dtype, int waves, const DrawArgs& a, int64_t n, hipStream_t s) {
+  return dtype == kF32 ? draw_of_type<kF32>(waves, a, n, s) : dtype == kF16 ? draw_of_type<kF16>(waves, a, n, s) : draw_of_type<kBF16>(waves, a, n, s);
+}
+
+hipError_t launch_draw_mass(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
+  return dtype == kF32 ? mass_of_type<kF32>(a, n, s) : dtype == kF16 ? mass_of_type<kF16>(a, n, s) : mass_of_type<kBF16>(a, n, s);
+}
+
+hipError_t launch_draw_join(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
+  return dtype == kF32 ? join_of_type<kF32>(a, n, s) : dtype == kF16 ? join_of_type<kF16>(a, n, s) : join_of_type<kBF16>(a, n, s);
 }
 
 }  // namespace rtopk
