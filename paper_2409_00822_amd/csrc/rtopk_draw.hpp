@@ -47,77 +47,64 @@ __device__ __forceinline__ double power2_finite(double t) {
 // The same with 0 for -inf; NaN stays.
 __device__ __forceinline__ double power2(double t) { return power2_finite(t < -1100.0 ? -1100.0 : t); }
 
-// f of the 64 lanes' values, the same in every lane.
-template <typename F>
-__device__ __forceinline__ double wave_reduce(double v, F f) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
+// A 64-bit value moved by a DPP permutation, 0 where it comes from no lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {
+  const long long b = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((long long)hi << 32 | (uint32_t)lo);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {  // lane: uniform
+  const long long b = __double_as_longlong(v);
+  return __longlong_as_double((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
+}
+// Inclusive sums over the lanes.
+__device__ __forceinline__ double wave_scan(double v) {
+  v += moved<0x111, 0xf>(v);  // row_shr:1
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);  // row_bcast:15
+  v += moved<0x143, 0xc>(v);  // row_bcast:31
   return v;
 }
-__device__ __forceinline__ double wave_sum(double v) {
-  return wave_reduce(v, [](double a, double b) { return a + b; });
-}
+// Sum of the lanes, the same in every lane.
+__device__ __forceinline__ double wave_sum(double v) { return lane_value(wave_scan(v), 63); }
 
-// A row's sum of powers about ref.  Nothing but -inf: s = 0; a NaN or +inf: s = NaN.
+// A row's (or a piece's) sum of powers about ref.  Nothing but -inf: s = 0; a NaN or +inf: s = NaN.
 struct Mass {
   double ref, s;
   __device__ __forceinline__ double power(float x, double c) const { return power2(((double)x - ref) * c); }
   __device__ __forceinline__ double over() const { return s == 0.0 ? 0.0 : 1.0 / s; }
 };
 
-// Columns [0, cols) from `row` on, for one wavefront: 128-bit chunks, chunk i for lane i mod 64, U at a time; then the chunks left and what is less than one.
-// Rows of 16-bit values that start at an odd one have their first column apart, as Segment has it.
-template <int DT>
-struct Piece {
-  using L = Logits<DT>;
-  Segment<DT> g;
-  __device__ __forceinline__ Piece(const typename L::elem* row, int cols) : g(row, cols) {}
-  // whole(chunks, U) for full batches, part(chunk) for single ones, which may hold -inf for what lies outside
-  template <int U, typename F, typename P>
-  __device__ __forceinline__ void each(int lane, F whole, P part) const {
-    int i = lane;
-    for (; i - lane + (U - 1) * 64 + 63 < g.full; i += U * 64) {
-      u4_vec w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = L::load(g.body + (uint32_t)(i + u * 64) * L::V);
-      whole(w);
-    }
-    for (; i < g.chunks(); i += 64) part(i < g.full ? L::load(g.body + (uint32_t)i * L::V) : g.partial());
-  }
-};
+// ---- pieces of rows -------------------------------------------------------------------------------
 
-// Sum of the powers about 0 of a piece, over the wavefront.  Masked columns make a first sum NaN; it is then taken again with -inf as the type's lowest
-// value, and so are all that follow.
-template <int DT>
-__device__ __forceinline__ double piece_sum(const typename Logits<DT>::elem* row, int cols, int lane, double c) {
+// A row is cut into pieces of a whole number of 128-bit loads of a wavefront (draw_pieces); a wavefront sums a piece, and what a row's pieces sum to says
+// which of them a draw falls in.
+
+// Sum of the powers about 0 of U chunks.  Masked columns make it NaN; it is then taken again with -inf as the type's lowest value, and so are all that follow.
+template <int DT, int U>
+__device__ __forceinline__ double chunk_powers(u4_vec (&w)[U], double c, bool& masked) {
   using L = Logits<DT>;
-  constexpr int U = DT == kF32 ? 4 : 2;
-  double s = 0.0;
-  bool masked = false;
-  const auto masked_power = [&](float x) { return power2_finite((double)(x == kNegInf ? -3.402823466e38f : x) * c); };
-  Piece<DT>(row, cols).template each<U>(
-      lane,
-      [&](u4_vec(&w)[U]) {
-        double a[2] = {0.0, 0.0};
-        if (!masked) {
+  double a[2] = {0.0, 0.0};
+  if (!masked) {
 #pragma unroll
-          for (int i = 0; i < U * L::V; ++i) a[i & 1] += power2_finite((double)L::at(w[i / L::V], i % L::V) * c);
-        }
-        if (masked || __any(!(a[0] + a[1] == a[0] + a[1]))) {
-          masked = true;
-          a[0] = a[1] = 0.0;
-          apart(w);
-          for (int u = 0; u < U; ++u)
+    for (int i = 0; i < U * L::V; ++i) a[i & 1] += power2_finite((double)L::at(w[i / L::V], i % L::V) * c);
+  }
+  if (masked || __any(!(a[0] + a[1] == a[0] + a[1]))) {
+    masked = true;
+    a[0] = a[1] = 0.0;
+    apart(w);
+#pragma unroll 1
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < L::V; ++i) a[i & 1] += masked_power(L::at(w[u], i));
-        }
-        s += a[0] + a[1];
-      },
-      [&](const u4_vec& w) {
-#pragma unroll
-        for (int i = 0; i < L::V; ++i) s += masked_power(L::at(w, i));
-      });
-  return wave_sum(s);
+      for (int i = 0; i < L::V; ++i) {
+        const float x = L::at(w[u], i);
+        a[i & 1] += power2_finite((double)(x == kNegInf ? -3.402823466e38f : x) * c);
+      }
+  }
+  return a[0] + a[1];
 }
 
 // f(column, value) for the thread's share of `cols` columns from `row` on, in 128-bit loads; i: the thread's number of T.
@@ -134,86 +121,107 @@ __device__ __forceinline__ void each_of(const typename Logits<DT>::elem* row, in
     for (int c = full * L::V; c < cols; ++c) f(c, L::widen(row[c]));
 }
 
-template <int W>
-struct DrawRoom {
-  double s[W];  // sums of the wavefronts' pieces, in order
-  float m[W];
-  uint64_t key[W];
-  int nan[W], past[W], last[W];
-};
-
-// Columns of each wavefront's piece of a row.
-template <int DT, int W>
-__device__ __forceinline__ int piece_cols(int cols) {
-  constexpr int V = Logits<DT>::V;
-  return ((cols + W - 1) / W + V - 1) / V * V;
-}
-
-// A row's (or segment's) mass, in every thread; the pieces' sums in room.s.
-template <int DT, int W>
-__device__ __forceinline__ Mass block_mass(const typename Logits<DT>::elem* row, int M, double c, DrawRoom<W>& room) {
-  constexpr int T = 64 * W;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int piece = piece_cols<DT, W>(M), from = min(wave * piece, M), cols = min(piece, M - from);
-  const auto join = [&](double s) {
-    if (lane == 0) room.s[wave] = s;
-    __syncthreads();
-    double all = 0.0;
+// The mass of a piece, in every lane of its wavefront.
+template <int DT>
+__device__ __forceinline__ Mass piece_mass(const typename Logits<DT>::elem* piece, int cols, int lane, double c) {
+  using L = Logits<DT>;
+  constexpr int U = DT == kF32 ? 4 : 2;
+  const Segment<DT> g(piece, cols);
+  double s = 0.0;
+  bool masked = false;
+  int i = lane;
+  for (; i - lane + U * 64 <= g.full; i += U * 64) {
+    u4_vec w[U];
 #pragma unroll
-    for (int w = 0; w < W; ++w) all += room.s[w];
-    return all;
-  };
-  const double s = piece_sum<DT>(row + from, cols, lane, c);
-  __syncthreads();
-  Mass t = {0.0, join(s)};
+    for (int u = 0; u < U; ++u) w[u] = L::load(g.body + (uint32_t)(i + u * 64) * L::V);
+    s += chunk_powers<DT, U>(w, c, masked);
+  }
+  for (; i - lane < g.chunks(); i += 64) {
+    u4_vec w[1] = {u4_vec{L::kLow, L::kLow, L::kLow, L::kLow}};
+    if (i < g.full) w[0] = L::load(g.body + (uint32_t)i * L::V);
+    else if (i == g.full) w[0] = g.partial();
+    masked |= i - lane + 64 > g.full;
+    s += chunk_powers<DT, 1>(w, c, masked);
+  }
+  Mass t = {0.0, wave_sum(s)};
   if (!(t.s >= kLeastSum && t.s <= kMostSum)) {  // about the maximum then
     float m = kNegInf;
-    each_of<DT>(row, M, threadIdx.x, T, [&](int, float x) { m = fmaxf(m, x); });
+    each_of<DT>(piece, cols, lane, 64, [&](int, float x) { m = fmaxf(m, x); });
     m = wave_max(m);
-    if (lane == 0) room.m[wave] = m;
-    __syncthreads();
-    for (int w = 0; w < W; ++w) m = fmaxf(m, room.m[w]);
     t.ref = m == kNegInf ? 0.0 : (double)m;
-    double u = 0.0;
-    each_of<DT>(row + from, cols, lane, 64, [&](int, float x) { u += t.power(x, c); });
-    t.s = join(wave_sum(u));
+    s = 0.0;
+    each_of<DT>(piece, cols, lane, 64, [&](int, float x) { s += t.power(x, c); });
+    t.s = wave_sum(s);
   }
   return t;
 }
 
-// Temperature 0: place_key of the largest logit, 0 where there is none, and whether there is a NaN; in every thread.
+// A row's mass from its pieces' (ref, s), in every lane; each wavefront for itself.
+__device__ __forceinline__ Mass join_mass(const double2* part, int pieces, double c) {
+  const int lane = threadIdx.x & 63;
+  Mass t = {0.0, 0.0};
+  for (int j = lane; j < pieces; j += 64) {
+    const double2 p = part[j];
+    if (p.y != 0.0) {  // (NaN too)
+      const double ref = t.s == 0.0 ? p.x : fmax(t.ref, p.x);
+      if (ref != t.ref && t.s != 0.0) t.s *= power2((t.ref - ref) * c);
+      t.s += ref == p.x ? p.y : p.y * power2((p.x - ref) * c);
+      t.ref = ref;
+    }
+  }
+  const uint64_t some = __ballot(t.s != 0.0);
+  if (some == 0) return {0.0, 0.0};
+  double ref = lane_value(t.ref, __builtin_ctzll(some));
+  if (__any(t.s != 0.0 && t.ref != ref)) {  // (seldom: all are about 0)
+    ref = t.s != 0.0 ? t.ref : -__builtin_inf();
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) ref = fmax(ref, __shfl_xor(ref, d));
+    if (t.s != 0.0 && t.ref != ref) t.s *= power2((t.ref - ref) * c);
+  }
+  return {ref, wave_sum(t.s)};
+}
+
+// Temperature 0: place_key of the largest logit, 0 where there is none, and whether there is a NaN.
 struct Best {
   uint64_t key;
   bool nan;
+  __device__ __forceinline__ void take(const Best& b) {
+    key = b.key > key ? b.key : key;
+    nan |= b.nan;
+  }
   __device__ __forceinline__ int col() const { return nan || key == 0 ? -1 : place_col(key); }
+  // (as a piece's mass is stored)
+  __device__ __forceinline__ double2 stored() const { return make_double2(nan ? 1.0 : 0.0, __longlong_as_double((long long)key)); }
+  static __device__ __forceinline__ Best from(const double2& p) { return {(uint64_t)__double_as_longlong(p.y), p.x != 0.0}; }
 };
 
-template <int DT, int W>
-__device__ __forceinline__ Best block_best(const typename Logits<DT>::elem* row, int first, int cols, DrawRoom<W>& room) {
-  constexpr int T = 64 * W;
+__device__ __forceinline__ Best wave_best(Best b) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) b.take({(uint64_t)__shfl_xor((unsigned long long)b.key, d), false});
+  b.nan = __any(b.nan);
+  return b;
+}
+
+template <int DT>
+__device__ __forceinline__ Best piece_best(const typename Logits<DT>::elem* row, int first, int cols, int lane) {
   Best b = {0, false};
-  each_of<DT>(row + first, cols, threadIdx.x, T, [&](int col, float x) {
-    const uint64_t key = x > kNegInf ? place_key(order_key(x), first + col) : 0;
-    b.key = key > b.key ? key : b.key;
+  float top = kNegInf;
+  int at = 0;
+  each_of<DT>(row + first, cols, lane, 64, [&](int col, float x) {
+    if (x > top) {  // (columns ascend)
+      top = x;
+      at = col;
+    }
     b.nan |= x != x;
   });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)b.key, d);
-    b.key = o > b.key ? o : b.key;
-  }
-  b.nan = __any(b.nan);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    room.key[threadIdx.x >> 6] = b.key;
-    room.nan[threadIdx.x >> 6] = b.nan;
-  }
-  __syncthreads();
-  for (int w = 0; w < W; ++w) {
-    b.key = room.key[w] > b.key ? room.key[w] : b.key;
-    b.nan |= room.nan[w] != 0;
-  }
-  return b;
+  if (top > kNegInf) b.key = place_key(order_key(top), first + at);
+  return wave_best(b);
+}
+
+__device__ __forceinline__ Best join_best(const double2* part, int pieces) {
+  Best b = {0, false};
+  for (int j = threadIdx.x & 63; j < pieces; j += 64) b.take(Best::from(part[j]));
+  return wave_best(b);
 }
 
 // ---- draws ----------------------------------------------------------------------------------------
@@ -252,14 +260,15 @@ __device__ __forceinline__ void each_weight(const Weights& w, const typename Log
   }
 }
 
-// Inclusive sums over the lanes.
-__device__ __forceinline__ double wave_scan(double v, int lane) {
+// A piece's weight, in every lane of its wavefront.
+template <int DT>
+__device__ __forceinline__ double piece_weight(const Weights& w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int first, int cols, int lane) {
+  double s = 0.0;
+  each_weight<DT>(w, p, q, first, cols, lane, 64, [&](const double(&v)[Logits<DT>::V], int) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
+    for (int c = 0; c < Logits<DT>::V; ++c) s += v[c];
+  });
+  return wave_sum(s);
 }
 
 // Of n pieces with the given sums, in order: the first that the cumulated sum passes `goal` in, or the last that has any; -1: none has.  before: the sum of
@@ -270,40 +279,41 @@ __device__ __forceinline__ int passing(int n, double goal, double& before, F sum
   double all = before;
   int at = -1;
   for (int j = 0; j < n; j += 64) {
-    const double s = j + lane < n ? sum(j + lane) : 0.0, to = all + wave_scan(s, lane);
+    const double s = j + lane < n ? sum(j + lane) : 0.0, to = all + wave_scan(s);
     const uint64_t have = __ballot(s > 0.0), past = __ballot(s > 0.0 && to > goal);
     if (have != 0) {
       const int l = past != 0 ? __builtin_ctzll(past) : 63 - __builtin_clzll(have);
       at = j + l;
-      before = __shfl(to - s, l);
+      before = lane_value(to - s, l);
     }
     if (past != 0) break;
-    all = __shfl(to, 63);
+    all = lane_value(to, 63);
   }
   return at;
 }
 
+template <int W>
+struct FindRoom {
+  double s[W];
+  int past[W], last[W];
+};
+
 // The column of [first, first + cols) that the cumulated weight, `before` at `first`, passes `goal` in, or the last that has any; in every thread.  Cut into a
-// piece for each wavefront, and the piece that it passes in again, until a thread has a chunk of it.
+// part for each wavefront, and the part that it passes in again, until a thread has a chunk of it.
 template <int DT, int W>
-__device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int first, int cols, double before, double goal, DrawRoom<W>& room) {
+__device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int first, int cols, double before, double goal, FindRoom<W>& room) {
   constexpr int V = Logits<DT>::V, T = 64 * W;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   while (cols > T * V) {
-    const int piece = piece_cols<DT, W>(cols), from = min(wave * piece, cols);
-    double s = 0.0;
-    each_weight<DT>(w, p, q, first + from, min(piece, cols - from), lane, 64, [&](const double(&v)[V], int) {
-#pragma unroll
-      for (int c = 0; c < V; ++c) s += v[c];
-    });
-    s = wave_sum(s);
+    const int part = ((cols + W - 1) / W + V - 1) / V * V, from = min(wave * part, cols);
+    const double s = piece_weight<DT>(w, p, q, first + from, min(part, cols - from), lane);
     __syncthreads();
     if (lane == 0) room.s[wave] = s;
     __syncthreads();
     const int j = passing(W, goal, before, [&](int i) { return room.s[i]; });
     if (j < 0) return -1;
-    first += j * piece;
-    cols = min(piece, cols - j * piece);
+    first += j * part;
+    cols = min(part, cols - j * part);
   }
   double v[V], s = 0.0;
   int col = 0;
@@ -317,20 +327,20 @@ __device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, 
     }
     col = at;
   });
-  double to = wave_scan(s, lane);
+  double to = wave_scan(s);
   __syncthreads();
   if (lane == 63) room.s[wave] = to;
   __syncthreads();
-  for (int j = 0; j < wave; ++j) before += room.s[j];
+#pragma unroll
+  for (int j = 0; j < W; ++j) before += j < wave ? room.s[j] : 0.0;
   to += before;
   const uint64_t have = __ballot(s > 0.0), past = __ballot(s > 0.0 && to > goal);
   const int one = past != 0 ? __builtin_ctzll(past) : 63 - __builtin_clzll(have | 1);
   if (lane == one) {
     double sum = to - s;
-    int at = -1;
+    int at = 0;
 #pragma unroll
-    for (int c = V - 1; c >= 0; --c)
-      if (at < 0 && v[c] > 0.0) at = c;  // the last
+    for (int c = 0; c < V; ++c) at = v[c] > 0.0 ? c : at;  // the last
     bool found = false;
 #pragma unroll
     for (int c = 0; c < V; ++c) {
@@ -345,57 +355,62 @@ __device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, 
   }
   __syncthreads();
   int at = -1;
-  for (int j = W - 1; j >= 0; --j)
-    if (at < 0) at = room.last[j];
-  for (int j = W - 1; j >= 0; --j)
-    if (room.past[j] >= 0) at = room.past[j];
+#pragma unroll
+  for (int j = 0; j < W; ++j) at = room.last[j] >= 0 ? room.last[j] : at;
+#pragma unroll
+  for (int j = W - 1; j >= 0; --j) at = room.past[j] >= 0 ? room.past[j] : at;
   return at;
 }
 
-// A draw by u from the weights of a row's columns, the pieces' sums known (`summed`: in room.s, of p about w.p.ref) or not.  Draws from p where the weights' whole
-// is no more than kLeastMass.
+// A draw by u from the weights of a row: rest[j] are its pieces' sums where they are p - q, else part[j] their masses in p.  Draws from p where the weights'
+// whole is no more than kLeastMass.
 template <int DT, int W>
-__device__ int block_draw(Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int M, double u, bool summed, DrawRoom<W>& room) {
-  constexpr int V = Logits<DT>::V;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int piece = piece_cols<DT, W>(M), from = min(wave * piece, M), cols = min(piece, M - from);
+__device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, const double2* part, const double* rest, double u,
+                          FindRoom<W>& room) {
+  const int lane = threadIdx.x & 63;
+  const auto cols = [&](int j) { return min(a.piece_cols, a.M - j * a.piece_cols); };
+  // the piece with the draft that stood for itself, without it; each wavefront for itself
+  const int special = w.without >= 0 ? w.without / a.piece_cols : -1;
+  const double special_sum = special >= 0 ? piece_weight<DT>(w, p, q, special * a.piece_cols, cols(special), lane) : 0.0;
   for (;;) {
-    const bool part = w.less || !summed || (w.without >= from && w.without < from + cols);
-    double s = 0.0;
-    if (part) {
-      each_weight<DT>(w, p, q, from, cols, lane, 64, [&](const double(&v)[V], int) {
-#pragma unroll
-        for (int c = 0; c < V; ++c) s += v[c];
-      });
-      s = wave_sum(s);
-    } else {
-      s = room.s[wave] * w.over_p;
-    }
-    __syncthreads();
-    if (lane == 0) room.s[wave] = s;
-    __syncthreads();
+    const auto sum = [&](int j) {
+      if (w.less) return rest[j];
+      if (w.without >= 0 && j == special) return special_sum;
+      const double2 t = part[j];
+      return t.y * (t.x == w.p.ref || t.y == 0.0 ? 1.0 : power2((t.x - w.p.ref) * w.c)) * w.over_p;
+    };
     double all = 0.0;
-#pragma unroll
-    for (int j = 0; j < W; ++j) all += room.s[j];
+    for (int j = lane; j < a.pieces; j += 64) all += sum(j);
+    all = wave_sum(all);
     if ((w.less || w.without >= 0) && !(all > kLeastMass)) {
       w.less = false;
       w.without = -1;
-      summed = false;
       continue;
     }
     if (!(all > 0.0)) return -1;
     const double goal = fmax(u * all, 0.0);  // (NaN: 0)
     double before = 0.0;
-    const int j = passing(W, goal, before, [&](int i) { return room.s[i]; });
-    if (j < 0) return -1;
-    return block_find<DT, W>(w, p, q, j * piece, min(piece, M - j * piece), before, goal, room);
+    const int j = passing(a.pieces, goal, before, sum);
+    return j < 0 ? -1 : block_find<DT, W>(w, p, q, j * a.piece_cols, cols(j), before, goal, room);
   }
 }
+
+// ---- sequences ------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int draft_at(const DrawArgs& a, int64_t n, int pos) {  // -1: none
   if (pos >= a.G) return -1;
   const int64_t i = n * a.G + pos, t = a.token64 ? static_cast<const int64_t*>(a.drafts)[i] : static_cast<const int32_t*>(a.drafts)[i];
   return t >= 0 && t < a.M ? (int)t : -1;
+}
+
+// How many drafts a sequence has; each wavefront for itself.
+__device__ __forceinline__ int drafts_of(const DrawArgs& a, int64_t n) {
+  const int lane = threadIdx.x & 63;
+  for (int j = 0; j < a.G; j += 64) {
+    const uint64_t none = __ballot(j + lane >= a.G || draft_at(a, n, j + lane) < 0);
+    if (none != 0) return j + __builtin_ctzll(none);
+  }
+  return a.G;
 }
 
 __device__ __forceinline__ void write_token(const DrawArgs& a, int64_t i, int token) {
@@ -409,59 +424,13 @@ __device__ __forceinline__ void write_sequence(const DrawArgs& a, int64_t n, int
   if (threadIdx.x == 0 && a.accepted) a.accepted[n] = accepted;
 }
 
-// A sequence's temperature, its factor, and what is to be done with it.
+// A sequence's temperature and its factor.
 struct Heat {
   double T, c;
   __device__ __forceinline__ Heat(const DrawArgs& a, int64_t n) : T(a.temperatures ? (double)a.temperatures[n] : a.temperature), c(kLog2e64 / T) {}
   __device__ __forceinline__ bool certain() const { return T == 0.0; }
   __device__ __forceinline__ bool none() const { return !(T >= 0.0 && T < __builtin_inf()); }
 };
-
-// One workgroup takes a sequence: its rows one after the other until a draft is rejected, then the draw.
-template <int DT, int W>
-__global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
-  using elem = typename Logits<DT>::elem;
-  __shared__ DrawRoom<W> room;
-  const int64_t n = a.row0 + blockIdx.x;
-  const Heat heat(a, n);
-  const auto* target = static_cast<const elem*>(a.target) + n * a.target_seq;
-  const auto* draft = static_cast<const elem*>(a.draft) + (a.draft ? n * a.draft_seq : 0);
-  int pos = 0, drawn = -1;
-  if (heat.certain()) {
-    for (;; ++pos) {
-      drawn = block_best<DT, W>(target + pos * a.target_pos, 0, a.M, room).col();
-      if (drawn < 0 || draft_at(a, n, pos) != drawn) break;
-    }
-  } else if (!heat.none()) {
-    Weights w;
-    w.c = heat.c;
-    const elem *p, *q;
-    for (;; ++pos) {
-      p = target + pos * a.target_pos;
-      q = draft + pos * a.draft_pos;
-      w.p = block_mass<DT, W>(p, a.M, w.c, room);
-      w.over_p = w.p.over();
-      w.without = -1;
-      w.less = false;
-      const int d = draft_at(a, n, pos);
-      if (d < 0) break;
-      double q_d = 1.0;
-      if (a.draft) {
-        w.q = block_mass<DT, W>(q, a.M, w.c, room);
-        w.over_q = w.q.over();
-        q_d = w.q.power(Logits<DT>::widen(q[d]), w.c) * w.over_q;
-        w.less = true;
-      } else {
-        w.without = d;
-      }
-      if (!((double)a.uniforms[n * (a.G + 1) + pos] * q_d < w.p.power(Logits<DT>::widen(p[d]), w.c) * w.over_p)) break;
-    }
-    if (w.is_number()) drawn = block_draw<DT, W>(w, p, q, a.M, (double)a.uniforms[n * (a.G + 1) + a.G], !w.less, room);
-  }
-  write_sequence(a, n, pos, drawn, 64 * W);
-}
-
-// ---- few sequences, spread over workgroups ---------------------------------------------------------
 
 // Row `row` of a sequence's 2 G + 1: its target's rows first, then its draft's.
 template <int DT>
@@ -470,28 +439,94 @@ __device__ __forceinline__ const typename Logits<DT>::elem* row_of(const DrawArg
   return row <= a.G ? static_cast<const elem*>(a.target) + n * a.target_seq + row * a.target_pos
                     : static_cast<const elem*>(a.draft) + n * a.draft_seq + (row - a.G - 1) * a.draft_pos;
 }
+__device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.draft ? 2 * a.G + 1 : a.G + 1; }
 
-// How many drafts a sequence has; each wavefront for itself.
-__device__ __forceinline__ int drafts_of(const DrawArgs& a, int64_t n) {
-  const int lane = threadIdx.x & 63;
-  for (int j = 0; j < a.G; j += 64) {
-    const uint64_t none = __ballot(j + lane >= a.G || draft_at(a, n, j + lane) < 0);
-    if (none != 0) return j + __builtin_ctzll(none);
+// One workgroup takes a sequence: its rows one after the other until a draft is rejected, then the draw.
+template <int DT, int W>
+__global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
+  using elem = typename Logits<DT>::elem;
+  __shared__ FindRoom<W> room;
+  __shared__ double2 part[kMostPieces];
+  __shared__ double2 draft_part[kMostPieces];  // then the sums of p - q
+  const int64_t n = a.row0 + blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Heat heat(a, n);
+  const auto each_piece = [&](auto f) {
+    for (int j = wave; j < a.pieces; j += W) f(j, j * a.piece_cols, min(a.piece_cols, a.M - j * a.piece_cols));
+  };
+  int pos = 0, drawn = -1;
+  if (heat.certain()) {
+    for (;; ++pos) {
+      const elem* x = row_of<DT>(a, n, pos);
+      __syncthreads();
+      each_piece([&](int j, int first, int cols) {
+        const Best b = piece_best<DT>(x, first, cols, lane);
+        if (lane == 0) part[j] = b.stored();
+      });
+      __syncthreads();
+      drawn = join_best(part, a.pieces).col();
+      if (drawn < 0 || draft_at(a, n, pos) != drawn) break;
+    }
+  } else if (!heat.none()) {
+    Weights w;
+    w.c = heat.c;
+    const elem *p, *q;
+    const auto row_mass = [&](const elem* x, double2* to) {
+      __syncthreads();
+      each_piece([&](int j, int first, int cols) {
+        const Mass t = piece_mass<DT>(x + first, cols, lane, w.c);
+        if (lane == 0) to[j] = make_double2(t.ref, t.s);
+      });
+      __syncthreads();
+      return join_mass(to, a.pieces, w.c);
+    };
+    for (;; ++pos) {
+      p = q = row_of<DT>(a, n, pos);
+      w.p = row_mass(p, part);
+      w.over_p = w.p.over();
+      w.without = -1;
+      w.less = false;
+      const int d = draft_at(a, n, pos);
+      if (d < 0) break;
+      double q_d = 1.0;
+      if (a.draft) {
+        q = row_of<DT>(a, n, a.G + 1 + pos);
+        w.q = row_mass(q, draft_part);
+        w.over_q = w.q.over();
+        q_d = w.q.power(Logits<DT>::widen(q[d]), w.c) * w.over_q;
+        w.less = true;
+      } else {
+        w.without = d;
+      }
+      if (!((double)a.uniforms[n * (a.G + 1) + pos] * q_d < w.p.power(Logits<DT>::widen(p[d]), w.c) * w.over_p)) break;
+    }
+    if (w.is_number()) {
+      double* rest = reinterpret_cast<double*>(draft_part);
+      if (w.less) {
+        __syncthreads();
+        each_piece([&](int j, int first, int cols) {
+          const double s = piece_weight<DT>(w, p, q, first, cols, lane);
+          if (lane == 0) rest[j] = s;
+        });
+        __syncthreads();
+      }
+      drawn = block_draw<DT, W>(a, w, p, q, part, rest, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+    }
   }
-  return a.G;
+  write_sequence(a, n, pos, drawn, 64 * W);
 }
 
-// The mass of a segment of a row (at temperature 0: its best column) to scratch memory.  All rows that may be looked at, those behind a rejected draft
-// among them: their workgroups have the GPU to themselves otherwise.
+// ---- few sequences, spread over workgroups ---------------------------------------------------------
+
+// The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  All rows that may be looked at, those
+// behind a rejected draft among them: their workgroups have the GPU to themselves otherwise.
 template <int DT>
-__global__ __launch_bounds__(256) void draw_mass_kernel(DrawArgs a) {
-  constexpr int W = 4;
-  __shared__ DrawRoom<W> room;
-  const int seg = (int)(blockIdx.x % (uint32_t)a.segments), rows = a.draft ? 2 * a.G + 1 : a.G + 1;
-  const uint32_t of = blockIdx.x / (uint32_t)a.segments;
-  const int row = (int)(of % (uint32_t)rows);
-  const int64_t n = a.row0 + of / (uint32_t)rows;
-  if (seg == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
+__global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) {
+  const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves, of = blockIdx.x / groups, rows = (uint32_t)rows_of(a);
+  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, row = (int)(of % rows);
+  const int64_t n = a.row0 + of / rows;
+  if (a.arrived && blockIdx.x % groups == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
+  if (piece >= a.pieces) return;
   const Heat heat(a, n);
   if (heat.none() || (heat.certain() && row > a.G)) return;
   if (a.G > 0) {
@@ -499,79 +534,42 @@ __global__ __launch_bounds__(256) void draw_mass_kernel(DrawArgs a) {
     if (row <= a.G ? row > g : row - a.G - 1 >= g) return;
   }
   const auto* x = row_of<DT>(a, n, row);
-  const int first = seg * a.seg_cols, cols = min(a.seg_cols, a.M - first);
+  const int first = piece * a.piece_cols, cols = min(a.piece_cols, a.M - first);
   double2 out;
   if (heat.certain()) {
-    const Best b = block_best<DT, W>(x, first, cols, room);
-    out = make_double2(b.nan ? 1.0 : 0.0, __longlong_as_double((long long)b.key));
+    out = piece_best<DT>(x, first, cols, lane).stored();
   } else {
-    const Mass t = block_mass<DT, W>(x + first, cols, heat.c, room);
+    const Mass t = piece_mass<DT>(x + first, cols, lane, heat.c);
     out = make_double2(t.ref, t.s);
   }
-  if (threadIdx.x == 0) a.part[(n * rows + row) * a.segments + seg] = out;
+  if (lane == 0) a.part[(n * rows + row) * a.pieces + piece] = out;
 }
 
-// A row's mass from its segments', in every lane.
-__device__ __forceinline__ Mass join_mass(const DrawArgs& a, int64_t n, int rows, int row, double c) {
-  const int lane = threadIdx.x & 63;
-  const double2* part = a.part + (n * rows + row) * a.segments;
-  Mass t = {0.0, 0.0};
-  for (int j = lane; j < a.segments; j += 64) {
-    const double2 p = part[j];
-    if (p.y != 0.0) {  // (NaN too)
-      const double ref = t.s == 0.0 ? p.x : fmax(t.ref, p.x);
-      if (ref != t.ref) t.s *= t.s == 0.0 ? 1.0 : power2((t.ref - ref) * c);
-      t.s += ref == p.x ? p.y : p.y * power2((p.x - ref) * c);
-      t.ref = ref;
-    }
-  }
-  const double ref = wave_reduce(t.s == 0.0 ? -__builtin_inf() : t.ref, [](double u, double v) { return fmax(u, v); });
-  if (ref == -__builtin_inf()) return {0.0, 0.0};
-  if (t.s != 0.0 && t.ref != ref) t.s *= power2((t.ref - ref) * c);
-  return {ref, wave_sum(t.s)};
-}
-
-__device__ __forceinline__ Best join_best(const DrawArgs& a, int64_t n, int rows, int row) {
-  const int lane = threadIdx.x & 63;
-  const double2* part = a.part + (n * rows + row) * a.segments;
-  Best b = {0, false};
-  for (int j = lane; j < a.segments; j += 64) {
-    const uint64_t key = (uint64_t)__double_as_longlong(part[j].y);
-    b.key = key > b.key ? key : b.key;
-    b.nan |= part[j].x != 0.0;
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)b.key, d);
-    b.key = o > b.key ? o : b.key;
-  }
-  b.nan = __any(b.nan);
-  return b;
-}
-
-// Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) each of `segments` workgroups takes a segment's sum of
-// it, and the last one of the sequence that is done (counted from 0, which draw_mass_kernel set) goes on; else the first one does it alone.  Which one is
-// last changes nothing: sums lie in memory and are taken in order.
+// Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
+// last one of them that is done (counted from 0, which draw_mass_kernel set) goes on; else the first one does it alone.  Which one is last changes
+// nothing: sums lie in memory and are taken in order.
 template <int DT>
-__global__ __launch_bounds__(256) void draw_join_kernel(DrawArgs a) {
+__global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) {
   using elem = typename Logits<DT>::elem;
-  constexpr int W = 4, T = 64 * W;
-  __shared__ DrawRoom<W> room;
+  constexpr int W = kDrawWaves, T = 64 * W;
+  __shared__ FindRoom<W> room;
   __shared__ double2 mass[2 * kMaxDrafts + 1];
   __shared__ int best[kMaxDrafts + 1], last;
-  const int parts = a.draft ? a.segments : 1, seg = (int)(blockIdx.x % (uint32_t)parts), rows = a.draft ? 2 * a.G + 1 : a.G + 1;
-  const int64_t n = a.row0 + blockIdx.x / (uint32_t)parts;
+  const uint32_t groups = a.draft ? (uint32_t)(a.pieces + W - 1) / W : 1;
+  const int group = (int)(blockIdx.x % groups), rows = rows_of(a);
+  const int64_t n = a.row0 + blockIdx.x / groups;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Heat heat(a, n);
   if (heat.none()) {
-    if (seg == 0) write_sequence(a, n, 0, -1, T);
+    if (group == 0) write_sequence(a, n, 0, -1, T);
     return;
   }
   const int g = a.G > 0 ? drafts_of(a, n) : 0;
+  const double2* parts = a.part + n * rows * a.pieces;
   if (heat.certain()) {
-    if (seg != 0) return;
+    if (group != 0) return;
     for (int row = wave; row <= g; row += W) {
-      const int col = join_best(a, n, rows, row).col();
+      const int col = join_best(parts + row * a.pieces, a.pieces).col();
       if (lane == 0) best[row] = col;
     }
     __syncthreads();
@@ -580,10 +578,9 @@ __global__ __launch_bounds__(256) void draw_join_kernel(DrawArgs a) {
     write_sequence(a, n, pos, best[pos], T);
     return;
   }
-  for (int i = wave; i < 2 * g + 1; i += W) {
+  for (int i = wave; i < (a.draft ? 2 * g + 1 : g + 1); i += W) {
     const int row = i <= g ? i : a.G + i - g;
-    if (row > a.G && !a.draft) break;
-    const Mass t = join_mass(a, n, rows, row, heat.c);
+    const Mass t = join_mass(parts + (int64_t)row * a.pieces, a.pieces, heat.c);
     if (lane == 0) mass[row] = make_double2(t.ref, t.s);
   }
   __syncthreads();
@@ -621,67 +618,28 @@ __global__ __launch_bounds__(256) void draw_join_kernel(DrawArgs a) {
     q = row_of<DT>(a, n, a.G + 1 + pos);
   }
   if (!w.is_number() || !w.less) {
-    if (seg != 0) return;
+    if (group != 0) return;
     if (!w.is_number()) {
       write_sequence(a, n, pos, -1, T);
       return;
     }
   }
-  const auto segment_cols = [&](int j) { return min(a.seg_cols, a.M - j * a.seg_cols); };
-  const auto weigh = [&](int j) {  // a segment's weight, over the workgroup
-    double s = 0.0;
-    each_weight<DT>(w, p, q, j * a.seg_cols, segment_cols(j), threadIdx.x, T, [&](const double(&v)[Logits<DT>::V], int) {
-#pragma unroll
-      for (int c = 0; c < Logits<DT>::V; ++c) s += v[c];
-    });
-    s = wave_sum(s);
-    __syncthreads();
-    if (lane == 0) room.s[wave] = s;
-    __syncthreads();
-    s = 0.0;
-#pragma unroll
-    for (int j = 0; j < W; ++j) s += room.s[j];
-    return s;
-  };
-  double* rest = a.rest + n * a.segments;
+  double* rest = a.rest + n * a.pieces;
   if (w.less) {
-    const double s = weigh(seg);
-    if (threadIdx.x == 0) {
-      __hip_atomic_store(rest + seg, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last = __hip_atomic_fetch_add(a.arrived + n, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    const int piece = group * W + wave, first = piece * a.piece_cols;
+    if (piece < a.pieces) {
+      const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
+      if (lane == 0) rest[piece] = s;
     }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.arrived + n, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)groups - 1;
     __syncthreads();
     if (!last) return;
+    __threadfence();
   }
-  double special = 0.0;  // the segment without the draft that stood for itself
-  const int special_seg = w.without >= 0 ? w.without / a.seg_cols : -1;
-  if (special_seg >= 0) special = weigh(special_seg);
-  for (;;) {
-    const double2* part = a.part + (n * rows + pos) * a.segments;
-    const auto sum = [&](int j) {
-      if (w.less) return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (j == special_seg && w.without >= 0) return special;
-      const double2 t = part[j];
-      return t.y * (t.x == w.p.ref || t.y == 0.0 ? 1.0 : power2((t.x - w.p.ref) * w.c)) * w.over_p;
-    };
-    double all = 0.0;
-    for (int j = lane; j < a.segments; j += 64) all += sum(j);
-    all = wave_sum(all);
-    if ((w.less || w.without >= 0) && !(all > kLeastMass)) {
-      w.less = false;
-      w.without = -1;
-      continue;
-    }
-    int drawn = -1;
-    if (all > 0.0) {
-      const double goal = fmax((double)a.uniforms[n * (a.G + 1) + a.G] * all, 0.0);  // (NaN: 0)
-      double before = 0.0;
-      const int j = passing(a.segments, goal, before, sum);
-      if (j >= 0) drawn = block_find<DT, W>(w, p, q, j * a.seg_cols, segment_cols(j), before, goal, room);
-    }
-    write_sequence(a, n, pos, drawn, T);
-    return;
-  }
+  const int drawn = block_draw<DT, W>(a, w, p, q, parts + (int64_t)pos * a.pieces, rest, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+  write_sequence(a, n, pos, drawn, T);
 }
 
 }  // namespace rtopk

@@ -82,21 +82,22 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool draft = draft_logits != nullptr;
   rtopk::DrawLayout l = rtopk::draw_layout(B, G, M, dtype, draft);
-  if (l.segments > 1 && (!workspace || workspace_bytes < rtopk::draw_workspace(B, G, draft, l))) l = rtopk::draw_layout_whole(B, M);
+  if (l.spread && (!workspace || workspace_bytes < rtopk::draw_workspace(B, G, draft, l))) l = rtopk::draw_layout_whole(B, M, dtype);
+  a.pieces = l.pieces;
+  a.piece_cols = l.cols;
   hipError_t err = hipSuccess;
   // launch(sequences) for slices whose workgroups fit one launch (2^31 threads)
   const auto sliced = [&](int64_t each, auto launch) {
     const int64_t most = (1 << 21) / each;
     for (a.row0 = 0; a.row0 < B && err == hipSuccess; a.row0 += most) err = launch(B - a.row0 < most ? B - a.row0 : most);
   };
-  if (l.segments > 1) {
-    a.segments = l.segments;
-    a.seg_cols = l.cols;
+  if (l.spread) {
     a.part = static_cast<double2*>(workspace);
-    a.rest = reinterpret_cast<double*>(a.part + B * rtopk::draw_rows(G, draft) * l.segments);
-    a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.segments);
-    sliced((int64_t)rtopk::draw_rows(G, draft) * l.segments, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
-    sliced(l.segments, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
+    a.rest = reinterpret_cast<double*>(a.part + B * rtopk::draw_rows(G, draft) * l.pieces);
+    a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
+    const int64_t groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
+    sliced(rtopk::draw_rows(G, draft) * groups, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
+    sliced(groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
   } else {
     sliced(1, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
   }

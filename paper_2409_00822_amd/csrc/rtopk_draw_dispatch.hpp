@@ -22,10 +22,10 @@ struct DrawArgs {
   int64_t B, row0;  // sequences; first one of the launch
   void* tokens;     // [B][G + 1], as the drafts
   int32_t* accepted;  // [B], optional
+  int pieces, piece_cols;  // of a row
   // sequences spread over workgroups
-  int segments, seg_cols;
-  double2* part;     // [B][rows][segments] masses; rows: G + 1 of the target, G of the draft
-  double* rest;      // [B][segments] sums of max(p - q, 0)
+  double2* part;     // [B][rows][pieces] masses; rows: G + 1 of the target, G of the draft
+  double* rest;      // [B][pieces] sums of max(p - q, 0)
   int32_t* arrived;  // [B]
 };
 

@@ -15,12 +15,12 @@ hipError_t draw_of_type(int waves, const DrawArgs& a, int64_t n, hipStream_t s) 
 
 template <int DT>
 hipError_t mass_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * draw_rows(a.G, a.draft != nullptr) * a.segments)), dim3(256), 0, s, a);
+  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * draw_rows(a.G, a.draft != nullptr) * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 template <int DT>
 hipError_t join_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  return launch_kernel(draw_join_kernel<DT>, dim3((uint32_t)(n * (a.draft ? a.segments : 1))), dim3(256), 0, s, a);
+  return launch_kernel(draw_join_kernel<DT>, dim3((uint32_t)(n * (a.draft ? ceil_div(a.pieces, kDrawWaves) : 1))), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 }  // namespace
