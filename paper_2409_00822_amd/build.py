@@ -19,7 +19,8 @@ SOURCES = ["rtopk_api.hip", "rtopk_inst_g4_exact.hip", "rtopk_inst_g4_early.hip"
            "rtopk_inst_block_var.hip",
            "rtopk_inst_block_dense.hip", "rtopk_inst_block_h16.hip", "rtopk_inst_backward.hip", "rtopk_inst_stream.hip",
            "rtopk_inst_split.hip", "rtopk_logits_api.hip", "rtopk_inst_logits.hip", "rtopk_inst_logits_grad.hip",
-           "rtopk_draw_api.hip", "rtopk_inst_draw.hip", "rtopk_balance_api.hip", "rtopk_inst_balance.hip"]
+           "rtopk_draw_api.hip", "rtopk_inst_draw.hip", "rtopk_balance_api.hip", "rtopk_inst_balance.hip",
+           "rtopk_inst_balance_grad.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -19,7 +19,8 @@
 
 namespace rtopk {
 
-constexpr int kFlush = 64;  // turns that fp32 sums run over
+constexpr int kFlush = 64;  // tokens of a lane that fp32 sums run over
+constexpr float kFarMaximum = 1024.0f;  // log2(e) times a maximum beyond this is too coarse a reference: differences from the maximum are taken first
 
 // f over each N lanes (a power of two), the same in all of them.
 template <int N, typename F>
@@ -29,8 +30,14 @@ __device__ __forceinline__ float lanes_reduce(float v, F f) {
   if constexpr (N >= 4) v = f(v, dpp(std::integral_constant<int, 0x4e>{}));   // quad_perm [2, 3, 0, 1]
   if constexpr (N >= 8) v = f(v, dpp(std::integral_constant<int, 0x141>{}));  // row_half_mirror
   if constexpr (N >= 16) v = f(v, dpp(std::integral_constant<int, 0x140>{})); // row_mirror
-  if constexpr (N >= 32) v = f(v, __shfl_xor(v, 16));
-  if constexpr (N >= 64) v = f(v, __shfl_xor(v, 32));
+  if constexpr (N >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (N >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   return v;
 }
 template <int N>
@@ -42,101 +49,152 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return lanes_reduce<N>(v, [](float a, float b) { return a + b; });
 }
 
-// The lane's columns of a token's row: chunk i of the lane is chunk `lane + i N` of the row.
-template <int DT, int N, int LOADS>
-struct RouterRow {
+// The columns of a token's row that a lane has: chunk i of the lane is chunk `sub + i N` of the row.  RAGGED: the row is no whole number of chunks; its last chunk is
+// moved back to end with it, and what that shares with the chunk before is held twice and counts once (`keep`).  Rows narrower than a chunk are loaded
+// by the element.
+template <int DT, int N, int LOADS, bool RAGGED>
+struct RouterLane {
   using L = Logits<DT>;
+  using elem = typename L::elem;
   static constexpr int V = L::V;
-  float x[LOADS][V];
-  static __device__ __forceinline__ int column(int sub, int i) { return (sub + i * N) * V; }
-  __device__ __forceinline__ void load(const typename L::elem* row, int E, int sub, bool is) {
+  int at[LOADS];  // first column of the chunk
+  bool has[LOADS];
+  float keep[LOADS][V];
+  __device__ __forceinline__ RouterLane(int E, int sub) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int c0 = column(sub, i);
-      if (is && c0 + V <= E) {
-        const u4_vec w = L::load_once(row + c0);
+      const int c0 = (sub + i * N) * V;
+      has[i] = c0 < E;
+      at[i] = RAGGED ? (E < V ? 0 : min(c0, E - V)) : c0;
 #pragma unroll
-        for (int c = 0; c < V; ++c) x[i][c] = L::at(w, c);
-      } else {
+      for (int c = 0; c < V; ++c) keep[i][c] = !RAGGED || (has[i] && at[i] + c >= c0 && at[i] + c < E) ? 1.0f : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void load(const elem* row, int E, u4_vec (&w)[LOADS]) const {
+    if (!RAGGED || E >= V) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) x[i][c] = is && c0 + c < E ? L::widen(row[c0 + c]) : kNegInf;
+      for (int i = 0; i < LOADS; ++i) {
+        w[i] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
+        if (has[i]) w[i] = L::load_once(row + at[i]);
+      }
+    } else {
+      typename L::elem v[V];
+#pragma unroll
+      for (int c = 0; c < V; ++c) v[c] = row[c < E ? c : 0];
+      w[0] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
+      if (has[0]) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          if constexpr (DT == kF32) w[0][c] = c < E ? __float_as_uint(v[c]) : L::kLow;
+          else if ((c & 1) == 0) w[0][c / 2] = c < E ? v[c] : L::kLow & 0xffffu;
+          else w[0][c / 2] |= (c < E ? (uint32_t)v[c] : L::kLow & 0xffffu) << 16;
+        }
       }
     }
   }
-  // x becomes the probabilities; the log-sum-exp (-inf for a row of nothing but -inf, whose probabilities are 0)
-  __device__ __forceinline__ float softmax() {
-    float m = x[0][0], s = 0.0f;
+  __device__ __forceinline__ float kept(float v, int i, int c) const { return RAGGED ? v * keep[i][c] : v; }
+};
+
+// A row's powers about its maximum in the lane's columns, and their sum.  One fused multiply-add and one exp2 to a logit: the rounding of the reference
+// m log2(e) is in all powers alike, and in the log-sum-exp that is formed about it.
+template <int DT, int N, int LOADS, bool RAGGED>
+struct RouterRow {
+  using R = RouterLane<DT, N, LOADS, RAGGED>;
+  using L = Logits<DT>;
+  static constexpr int V = L::V;
+  float e[LOADS][V], m, s;
+  __device__ __forceinline__ RouterRow(const R& r, u4_vec (&w)[LOADS]) {
+    m = L::largest(w[0]);
+#pragma unroll
+    for (int i = 1; i < LOADS; ++i) m = vmax(m, L::largest(w[i]));
+    m = lanes_max<N>(m);
+    if (m == kNegInf) m = 0.0f;
+    const float about = m * kLog2e;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-      for (int c = 0; c < V; ++c) m = vmax(m, x[i][c]);
-    m = lanes_max<N>(m);
-    const float about = m == kNegInf ? 0.0f : m;
+      for (int c = 0; c < V; ++c) e[i][c] = __builtin_amdgcn_exp2f(__builtin_fmaf(L::at(w[i], c), kLog2e, -about));
+    if (__any(fabsf(m) > kFarMaximum)) {
+      apart(w);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+        for (int c = 0; c < V; ++c)
+          if (fabsf(m) > kFarMaximum) e[i][c] = __builtin_amdgcn_exp2f((L::at(w[i], c) - m) * kLog2e);
+    }
+    s = 0.0f;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        x[i][c] = __builtin_amdgcn_exp2f((x[i][c] - about) * kLog2e);
-        s += x[i][c];
+        if (RAGGED) s = __builtin_fmaf(e[i][c], r.keep[i][c], s);
+        else s += e[i][c];
       }
     s = lanes_sum<N>(s);
-    const float over = s == 0.0f ? 0.0f : 1.0f / s;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-      for (int c = 0; c < V; ++c) x[i][c] *= over;
-    return s == 0.0f ? kNegInf : about + logf(s);
   }
 };
 
+// 1 / s of a sum of powers about the maximum (1 <= s <= kMaxExperts, or 0, or NaN), and the log-sum-exp, 0 for a row of nothing but -inf.
+__device__ __forceinline__ float over_of(float s) { return s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s); }
+__device__ __forceinline__ float lse_of(float m, float s) {
+  constexpr float kLn2 = 0.69314718055994530942f;
+  const float log2_s = __builtin_amdgcn_logf(s), v = fabsf(m) > kFarMaximum ? __builtin_fmaf(log2_s, kLn2, m) : (m * kLog2e + log2_s) * kLn2;
+  return s == 0.0f ? 0.0f : v;
+}
+
 __device__ __forceinline__ int pick_at(const BalanceArgs& a, int64_t i) {  // -1: none
   const int c = a.col_bytes == 1 ? static_cast<const uint8_t*>(a.cols)[i] : static_cast<const int32_t*>(a.cols)[i];
-  return c >= 0 && c < a.E ? c : -1;
+  return (uint32_t)c < (uint32_t)a.E ? c : -1;
 }
 
-// The results of a group from its sums; all threads of a workgroup.  sum_p(e), picks(e): of column e.
-template <int T, typename P, typename C>
-__device__ __forceinline__ void write_balance(const BalanceArgs& a, int g, double z, int counted, double* room, P sum_p, C picks) {
-  double dot = 0.0, all = 0.0;
-  const double over = counted > 0 ? 1.0 / counted : 0.0;
-  for (int e = threadIdx.x; e < a.E; e += T) {
-    const double mean = sum_p(e) * over;
-    const int n = picks(e);
-    if (a.probs) a.probs[(int64_t)g * a.E + e] = (float)mean;
-    a.counts[(int64_t)g * a.E + e] = n;
-    if (n > 0) dot += mean * n;  // (what was never picked adds nothing, whatever it is)
-    all += n;
-  }
+// Whether a token of the lane's row has any pick: `any` of its N lanes, given their ballot.
+template <int N>
+__device__ __forceinline__ bool any_lane(uint64_t ballot, int of) {
+  const uint64_t mask = N == 64 ? ~(uint64_t)0 : ((uint64_t)1 << (N % 64)) - 1;
+  return ((ballot >> (of * N)) & mask) != 0;
+}
+// The ballot of a wavefront whose tokens all have k picks in their first k lanes.
+template <int N>
+__device__ __forceinline__ uint64_t full_ballot(int k) {
+  const uint64_t row = k >= N ? (N == 64 ? ~(uint64_t)0 : ((uint64_t)1 << (N % 64)) - 1) : ((uint64_t)1 << k) - 1;
+  uint64_t all = 0;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    dot += __shfl_xor(dot, d);
-    all += __shfl_xor(all, d);
-  }
-  if ((threadIdx.x & 63) == 0) {
-    room[2 * (threadIdx.x >> 6)] = dot;
-    room[2 * (threadIdx.x >> 6) + 1] = all;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    dot = all = 0.0;
-    for (int w = 0; w < T / 64; ++w) {
-      dot += room[2 * w];
-      all += room[2 * w + 1];
-    }
-    a.loss[g] = all > 0.0 ? (float)(a.E * dot / all) : 0.0f;
-    if (a.z) a.z[g] = (float)(z * over);
-    a.counted[g] = counted;
-  }
+  for (int i = 0; i < 64; i += N) all |= row << i;
+  return all;
 }
 
-template <int DT, int N, int LOADS>
+// Loads of a lane that are made together.
+constexpr int balance_batch(int loads) { return loads == 1 ? 4 : (loads == 2 ? 2 : 1); }
+
+__device__ __forceinline__ double lanes_total(double v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// ---- loss -----------------------------------------------------------------------------------------
+
+// A column's results; returns what it adds to the group's loss before the factors.
+__device__ __forceinline__ double write_column(const BalanceArgs& a, int g, int e, double sum, int picks, int counted) {
+  const double mean = counted > 0 ? sum / counted : 0.0;
+  if (a.probs) a.probs[(int64_t)g * a.E + e] = (float)mean;
+  a.counts[(int64_t)g * a.E + e] = picks;
+  return picks > 0 ? mean * picks : 0.0;  // (what was never picked adds nothing, whatever it is)
+}
+
+__device__ __forceinline__ void write_group(const BalanceArgs& a, int g, double dot, double z, int counted, int picked) {
+  a.loss[g] = picked > 0 ? (float)(a.E * dot / picked) : 0.0f;
+  if (a.z) a.z[g] = counted > 0 ? (float)(z / counted) : 0.0f;
+  a.counted[g] = counted;
+}
+
+template <int DT, int N, int LOADS, bool RAGGED>
 __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs a) {
-  using R = RouterRow<DT, N, LOADS>;
-  constexpr int W = kBalanceWaves, T = 64 * W, PER = 64 / N, V = R::V, COLS = N * LOADS * V;
+  using R = RouterLane<DT, N, LOADS, RAGGED>;
+  constexpr int W = kBalanceWaves, T = 64 * W, PER = 64 / N, V = R::V, COLS = N * LOADS * V, U = balance_batch(LOADS);
   __shared__ double sums[W][COLS];
   __shared__ double z_sums[W];
-  __shared__ double room[2 * W];
-  __shared__ int picks[COLS], tokens[W];
+  __shared__ int picks[COLS], tokens[W], all_picks[W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % N, of = lane / N;
   const int g = blockIdx.x / a.per_group, part = blockIdx.x % a.per_group;
   const int64_t first = part * a.rows, end = first + a.rows < a.per ? first + a.rows : a.per, base = (int64_t)g * a.per;
@@ -145,11 +203,14 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
 #pragma unroll
     for (int w = 0; w < W; ++w) sums[w][e] = 0.0;
   }
+  if (part == 0 && threadIdx.x == 0 && a.arrived) a.arrived[g] = 0;
   __syncthreads();
-  const auto* x = static_cast<const typename Logits<DT>::elem*>(a.x) + base * a.stride;
+  const auto* x = static_cast<const typename R::elem*>(a.x) + base * a.stride;
+  const R r(a.E, sub);
+  const uint64_t full = full_ballot<N>(a.k);
   float p[LOADS][V] = {};
-  double z_all = 0.0;
-  int counted = 0, turns = 0;
+  double z = 0.0;
+  int counted = 0, picked = 0, turns = 0;  // (counts of the wavefront)
   const auto flush = [&] {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
@@ -158,106 +219,193 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
         float v = p[i][c];
 #pragma unroll
         for (int d = N; d < 64; d <<= 1) v += __shfl_xor(v, d);
-        if (of == 0) sums[wave][R::column(sub, i) + c] += v;
+        if (of == 0 && r.has[i] && (!RAGGED || r.keep[i][c] != 0.0f)) sums[wave][r.at[i] + c] += v;
         p[i][c] = 0.0f;
       }
   };
-  for (int64_t t0 = first + wave * PER; t0 < end; t0 += W * PER) {
-    const int64_t t = t0 + of;
-    R r;
-    r.load(x + t * a.stride, a.E, sub, t < end);
-    bool any = false;
-    if (t < end)
-      for (int j = sub; j < a.k; j += N) {
-        const int col = pick_at(a, (base + t) * a.k + j);
-        any |= col >= 0;
-        if (col >= 0) atomicAdd(&picks[col], 1);
+  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U) {
+    u4_vec w[U][LOADS];
+    int col[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * PER + of, in = t < end ? t : end - 1;
+      r.load(x + in * a.stride, a.E, w[u]);
+      col[u] = sub < a.k && t < end ? pick_at(a, (base + in) * a.k + sub) : -1;
+    }
+    float own_m = 0.0f, own_s = 0.0f;  // of the token whose number is the lane's
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * PER + of;
+      if (t - of >= end) break;  // (uniform)
+      bool any = col[u] >= 0;
+      uint64_t ballot = __ballot(any);
+      if (any) atomicAdd(&picks[col[u]], 1);
+      picked += __popcll(ballot);
+      RouterRow<DT, N, LOADS, RAGGED> row(r, w[u]);
+      float over = over_of(row.s);
+      if (ballot == full && a.k <= N) {
+        counted += PER;
+      } else {
+        for (int j = sub + N; j - sub < a.k; j += N) {
+          const int more = j < a.k && t < end ? pick_at(a, (base + t) * a.k + j) : -1;
+          if (more >= 0) atomicAdd(&picks[more], 1);
+          const uint64_t b = __ballot(more >= 0);
+          picked += __popcll(b);
+          ballot |= b;
+        }
+        const bool counts = any_lane<N>(ballot, of);
+        counted += __popcll(__ballot(counts && sub == 0));
+        if (!counts) {  // (padding may hold NaN)
+          row.s = row.m = over = 0.0f;
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+            for (int c = 0; c < V; ++c) row.e[i][c] = 0.0f;
+        }
       }
-    const uint64_t mask = N == 64 ? ~(uint64_t)0 : ((uint64_t)1 << (N % 64)) - 1;
-    const bool counts = ((__ballot(any) >> (of * N)) & mask) != 0;
-    const float lse = r.softmax();
-    if (counts) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-        for (int c = 0; c < V; ++c) p[i][c] += r.x[i][c];
-      if (sub == 0) {
-        if (lse != kNegInf) z_all = __builtin_fma((double)lse, (double)lse, z_all);
-        ++counted;
+        for (int c = 0; c < V; ++c) p[i][c] = __builtin_fmaf(row.e[i][c], over, p[i][c]);
+      if constexpr (N >= U) {
+        own_m = sub == u ? row.m : own_m;
+        own_s = sub == u ? row.s : own_s;
+      } else {
+        const double lse = sub == 0 ? (double)lse_of(row.m, row.s) : 0.0;
+        z = __builtin_fma(lse, lse, z);
       }
     }
-    if (++turns % kFlush == 0) flush();
+    if constexpr (N >= U) {
+      const double lse = lse_of(own_m, own_s);
+      z = __builtin_fma(lse, lse, z);
+    }
+    turns += U;
+    if (turns >= kFlush) {
+      flush();
+      turns = 0;
+    }
   }
   flush();
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    z_all += __shfl_xor(z_all, d);
-    counted += __shfl_xor(counted, d);
-  }
+  z = lanes_total(z);
   if (lane == 0) {
-    z_sums[wave] = z_all;
+    z_sums[wave] = z;
     tokens[wave] = counted;
+    all_picks[wave] = picked;
   }
   __syncthreads();
-  z_all = 0.0;
-  counted = 0;
+  z = 0.0;
+  counted = picked = 0;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    z_all += z_sums[w];
+    z += z_sums[w];
     counted += tokens[w];
+    picked += all_picks[w];
   }
-  const auto sum_p = [&](int e) {
+  double dot = 0.0;
+  for (int e = threadIdx.x; e < a.E; e += T) {
     double v = 0.0;
 #pragma unroll
     for (int w = 0; w < W; ++w) v += sums[w][e];
-    return v;
-  };
-  if (a.per_group == 1) {
-    write_balance<T>(a, g, z_all, counted, room, sum_p, [&](int e) { return picks[e]; });
-  } else {
-    for (int e = threadIdx.x; e < a.E; e += T) {
-      a.part_p[(int64_t)blockIdx.x * a.E + e] = sum_p(e);
+    if (a.per_group == 1) {
+      dot += write_column(a, g, e, v, picks[e], counted);
+    } else {
+      a.part_p[(int64_t)blockIdx.x * a.E + e] = v;
       a.part_n[(int64_t)blockIdx.x * a.E + e] = picks[e];
     }
+  }
+  if (a.per_group == 1) {
+    dot = lanes_total(dot);
+    __syncthreads();
+    if (lane == 0) z_sums[wave] = dot;
+    __syncthreads();
     if (threadIdx.x == 0) {
-      a.part_z[blockIdx.x] = z_all;
-      a.part_rows[blockIdx.x] = counted;
+      dot = 0.0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) dot += z_sums[w];
+      write_group(a, g, dot, z, counted, picked);
     }
+  } else if (threadIdx.x == 0) {
+    a.part_z[blockIdx.x] = BalancePart{z, counted, picked};
   }
 }
 
-// Joins a group's workgroups, in order.
-template <int T>
+// Joins a group's workgroups, in order: C columns by a workgroup, its threads in slices of the parts.  The last of a group's that is done (counted from 0, which
+// balance_kernel set) adds up what each has for the loss, in order.  What it reads of the others is stored and loaded past the caches, so that no cache
+// has to be written back, which takes 5 us.
+template <int T, int C>
 __global__ __launch_bounds__(T) void balance_join_kernel(BalanceArgs a) {
-  __shared__ double p[kMaxExperts], room[T / 32];
-  __shared__ int n[kMaxExperts];
-  __shared__ double z;
-  __shared__ int counted;
-  const int g = blockIdx.x;
+  constexpr int S = T / C, W = T / 64;
+  __shared__ double p[S][C], of_wave[2][W];
+  __shared__ int n[S][C], counts[2][W];
+  const int blocks = (a.E + C - 1) / C, g = blockIdx.x / blocks, block = blockIdx.x % blocks;
+  const int slice = threadIdx.x / C, c = threadIdx.x % C, e = block * C + c, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t at = (int64_t)g * a.per_group;
-  for (int e = threadIdx.x; e < a.E; e += T) {
-    double s = 0.0;
-    int c = 0;
-    for (int j = 0; j < a.per_group; ++j) {
+  double s = 0.0, z = 0.0;
+  int k = 0, counted = 0, picked = 0;
+  if (e < a.E) {
+#pragma unroll 4
+    for (int j = slice; j < a.per_group; j += S) {
       s += a.part_p[(at + j) * a.E + e];
-      c += a.part_n[(at + j) * a.E + e];
+      k += a.part_n[(at + j) * a.E + e];
     }
-    p[e] = s;
-    n[e] = c;
   }
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    int c = 0;
-    for (int j = 0; j < a.per_group; ++j) {
-      s += a.part_z[at + j];
-      c += a.part_rows[at + j];
-    }
-    z = s;
-    counted = c;
+  for (int j = threadIdx.x; j < a.per_group; j += T) {
+    const BalancePart q = a.part_z[at + j];
+    z += q.z;
+    counted += q.counted;
+    picked += q.picked;
+  }
+  z = lanes_total(z);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    counted += __shfl_xor(counted, d);
+    picked += __shfl_xor(picked, d);
+  }
+  if (lane == 0) {
+    of_wave[0][wave] = z;
+    counts[0][wave] = counted;
+    counts[1][wave] = picked;
+  }
+  if (S > 1) {
+    p[slice][c] = s;
+    n[slice][c] = k;
   }
   __syncthreads();
-  write_balance<T>(a, g, z, counted, room, [&](int e) { return p[e]; }, [&](int e) { return n[e]; });
+  z = 0.0;
+  counted = picked = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    z += of_wave[0][w];
+    counted += counts[0][w];
+    picked += counts[1][w];
+  }
+  double dot = 0.0;
+  if (slice == 0 && e < a.E) {
+#pragma unroll
+    for (int i = 1; i < S; ++i) {
+      s += p[i][c];
+      k += n[i][c];
+    }
+    dot = write_column(a, g, e, s, k, counted);
+  }
+  dot = lanes_total(dot);
+  if (lane == 0) of_wave[1][wave] = dot;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  dot = 0.0;
+  for (int w = 0; w < W; ++w) dot += of_wave[1][w];
+  if (blocks > 1) {
+    double* dots = a.part_dot + (int64_t)g * blocks;
+    __hip_atomic_store(dots + block, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");  // (the store is done)
+    if (__hip_atomic_fetch_add(a.arrived + g, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != blocks - 1) return;
+    dot = 0.0;
+    for (int i = 0; i < blocks; ++i) dot += __hip_atomic_load(dots + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  write_group(a, g, dot, z, counted, picked);
 }
+
+// ---- gradient -------------------------------------------------------------------------------------
 
 // LDS of one wavefront: what it writes there it reads again itself, in the order of the program.
 __device__ __forceinline__ void wave_fence() {
@@ -265,97 +413,163 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-template <int DT, int N, int LOADS, bool VALS>
+// The picked values' gradients at their columns of the wavefront's tokens, 0 elsewhere: as the lanes hold the columns, in planes of four so that the
+// lanes' 128-bit reads meet no bank twice.  A column that two lanes hold is written for both.
+template <int DT, int N, int LOADS, bool RAGGED>
+struct PickedTile {
+  static constexpr int V = Logits<DT>::V, PER = 64 / N, PLANE = N * LOADS * 4;
+  float (&at)[PER][V / 4][PLANE];
+  int E, of;
+  __device__ __forceinline__ float& place(int chunk, int c) const { return at[of][c / 4][chunk * 4 + c % 4]; }
+  __device__ __forceinline__ void put(int col, float v) const {
+    const int last = (E - 1) / V;  // the chunk that ends with the row
+    if (!RAGGED || E < V || col / V != last) place(col / V, col % V) = v;
+    if (RAGGED && E >= V && col >= E - V) place(last, col - (E - V)) = v;
+  }
+  __device__ __forceinline__ void get(int chunk, float (&v)[V]) const {
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+      const float4 f = *reinterpret_cast<const float4*>(&at[of][h][chunk * 4]);
+      v[4 * h] = f.x;
+      v[4 * h + 1] = f.y;
+      v[4 * h + 2] = f.z;
+      v[4 * h + 3] = f.w;
+    }
+  }
+};
+
+template <int DT, int N, int LOADS, bool VALS, bool RAGGED>
 __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(BalanceArgs a) {
-  using R = RouterRow<DT, N, LOADS>;
+  using R = RouterLane<DT, N, LOADS, RAGGED>;
   using L = Logits<DT>;
-  constexpr int W = kBalanceWaves, PER = 64 / N, V = R::V, COLS = N * LOADS * V;
-  __shared__ float tile[VALS ? W : 1][VALS ? PER : 1][VALS ? COLS : 1];  // the picked values' gradients at their columns, 0 elsewhere
+  using Tile = PickedTile<DT, N, LOADS, RAGGED>;
+  constexpr int W = kBalanceWaves, PER = 64 / N, V = R::V, U = balance_batch(LOADS);
+  __shared__ __align__(16) float tiles[VALS ? W : 1][PER][V / 4][Tile::PLANE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % N, of = lane / N;
   const int g = blockIdx.x / a.per_group, part = blockIdx.x % a.per_group;
   const int64_t first = part * a.rows, end = first + a.rows < a.per ? first + a.rows : a.per, base = (int64_t)g * a.per;
   const auto* x = static_cast<const typename L::elem*>(a.x) + base * a.stride;
   auto* out = static_cast<typename L::elem*>(a.grad_x) + base * a.grad_stride;
+  const R r(a.E, sub);
+  const uint64_t full = full_ballot<N>(a.k);
   // w_e of the lane's columns
   float w[LOADS][V];
   double all = 0.0;
   for (int e = lane; e < a.E; e += 64) all += a.counts_in[(int64_t)g * a.E + e];
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+  all = lanes_total(all);
   const int tokens = a.counted_in[g];
-  const double over = tokens > 0 ? 1.0 / tokens : 0.0, each = all > 0.0 ? a.E * (double)a.grad_loss[g] * over / all : 0.0;
-  const float z2 = a.grad_z ? (float)(2.0 * a.grad_z[g] * over) : 0.0f;
+  const double over_n = tokens > 0 ? 1.0 / tokens : 0.0, each = all > 0.0 ? a.E * (double)a.grad_loss[g] * over_n / all : 0.0;
+  const float z2 = a.grad_z ? (float)(2.0 * a.grad_z[g] * over_n) : 0.0f;
 #pragma unroll
   for (int i = 0; i < LOADS; ++i)
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const int e = R::column(sub, i) + c;
+      const int e = r.at[i] + c;
       w[i][c] = e < a.E ? (float)(each * a.counts_in[(int64_t)g * a.E + e]) : 0.0f;
     }
+  const Tile tile{tiles[VALS ? wave : 0], a.E, of};
   if constexpr (VALS) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-      for (int c = 0; c < V; ++c) tile[wave][of][R::column(sub, i) + c] = 0.0f;
+    for (int c = lane; c < PER * V / 4 * Tile::PLANE; c += 64) (&tiles[wave][0][0][0])[c] = 0.0f;
     wave_fence();
   }
-  for (int64_t t0 = first + wave * PER; t0 < end; t0 += W * PER) {
-    const int64_t t = t0 + of;
-    R r;
-    r.load(x + t * a.stride, a.E, sub, t < end);
-    bool any = false;
-    if (t < end)
-      for (int j = sub; j < a.k; j += N) {
-        const int col = pick_at(a, (base + t) * a.k + j);
-        any |= col >= 0;
-        if (VALS && col >= 0) {
-          // the first entry of a column adds up all that have it
-          float v = a.grad_vals[(base + t) * a.k + j];
-          bool earlier = false;
-          for (int i = 0; i < a.k; ++i)
-            if (i != j && pick_at(a, (base + t) * a.k + i) == col) {
-              earlier |= i < j;
-              v += a.grad_vals[(base + t) * a.k + i];
-            }
-          if (!earlier) tile[wave][of][col] = v;
-        }
+  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U) {
+    u4_vec raw[U][LOADS];
+    int col[U];
+    float val[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * PER + of, in = t < end ? t : end - 1;
+      r.load(x + in * a.stride, a.E, raw[u]);
+      col[u] = -1;
+      if (sub < a.k && t < end) {
+        col[u] = pick_at(a, (base + in) * a.k + sub);
+        if (VALS) val[u] = a.grad_vals[(base + in) * a.k + sub];
       }
-    const uint64_t mask = N == 64 ? ~(uint64_t)0 : ((uint64_t)1 << (N % 64)) - 1;
-    const bool counts = ((__ballot(any) >> (of * N)) & mask) != 0;
-    if constexpr (VALS) wave_fence();
-    const float lse = r.softmax();
-    float dot = 0.0f;
+    }
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * PER + of, entry = (base + t) * a.k;
+      if (t - of >= end) break;  // (uniform)
+      uint64_t ballot = __ballot(col[u] >= 0);
+      bool counts = true, once = true;  // once: picks that ascend, so that none is there twice
+      if (VALS) {
+        const int before = __builtin_amdgcn_update_dpp(0, col[u], 0x138, 0xf, 0xf, false);  // wave_shr:1
+        once = !__any(col[u] >= 0 && sub > 0 && !(before >= 0 && before < col[u]));
+      }
+      if (!(ballot == full && a.k <= N)) {
+        for (int j = sub + N; j - sub < a.k; j += N) {
+          const int mine = j < a.k && t < end ? pick_at(a, entry + j) : -1;
+          ballot |= __ballot(mine >= 0);
+          if (VALS) {
+            const int before = mine >= 0 ? pick_at(a, entry + j - 1) : -1;
+            once = once && !__any(mine >= 0 && !(before >= 0 && before < mine));
+          }
+        }
+        counts = any_lane<N>(ballot, of);
+      }
+      // f(column, the gradients that it gets) for the picks of the lane
+      const auto picked = [&](auto f) {
+        if (once) {
+          if (col[u] >= 0) f(col[u], val[u]);
+          if (a.k > N && t < end)
+            for (int j = sub + N; j < a.k; j += N) {
+              const int mine = pick_at(a, entry + j);
+              if (mine >= 0) f(mine, a.grad_vals[entry + j]);
+            }
+        } else if (t < end) {
+          for (int j = sub; j < a.k; j += N) {
+            const int mine = pick_at(a, entry + j);
+            if (mine < 0) continue;
+            float v = a.grad_vals[entry + j];  // the first entry of a column adds up all that have it
+            bool earlier = false;
+            for (int i = 0; i < a.k; ++i)
+              if (i != j && pick_at(a, entry + i) == mine) {
+                earlier |= i < j;
+                v += a.grad_vals[entry + i];
+              }
+            if (!earlier) f(mine, v);
+          }
+        }
+      };
+      if constexpr (VALS) {
+        picked([&](int c, float v) { tile.put(c, v); });
+        wave_fence();
+      }
+      const RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
+      const float over = over_of(row.s);
+      float dot = 0.0f;
 #pragma unroll
-      for (int c = 0; c < V; ++c) dot = __builtin_fmaf(r.x[i][c], w[i][c], dot);
-    dot = lanes_sum<N>(dot);
-    const float both = (lse == kNegInf ? 0.0f : z2 * lse) - dot;
-    if (t < end) {
+      for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+        for (int c = 0; c < V; ++c) dot = __builtin_fmaf(r.kept(row.e[i][c], i, c), w[i][c], dot);
+      dot = lanes_sum<N>(dot) * over;
+      const float both = ((z2 == 0.0f ? 0.0f : z2 * lse_of(row.m, row.s)) - dot) * over;
       auto* to = out + t * a.grad_stride;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        const int c0 = R::column(sub, i);
-        float d[V];
+        float d[V], v[V];
+        if (VALS) tile.get(sub + i * N, v);
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          d[c] = counts ? r.x[i][c] * (w[i][c] + both) : 0.0f;
-          if (VALS) d[c] += tile[wave][of][c0 + c];
+          d[c] = row.e[i][c] * __builtin_fmaf(w[i][c], over, both);
+          if (!counts) d[c] = 0.0f;
+          if (VALS) d[c] += v[c];
         }
-        if (c0 + V <= a.E) L::store(to + c0, L::pack(d));
-        else
-          for (int c = 0; c < V; ++c)
-            if (c0 + c < a.E) to[c0 + c] = L::narrow(d[c]);
+        if (t < end && r.has[i]) {
+          if (!RAGGED || a.E >= V) {
+            L::store(to + r.at[i], L::pack(d));
+          } else {
+#pragma unroll
+            for (int c = 0; c < V; ++c)
+              if (c < a.E) to[c] = L::narrow(d[c]);
+          }
+        }
       }
-    }
-    if constexpr (VALS) {
-      wave_fence();
-      if (t < end)
-        for (int j = sub; j < a.k; j += N) {
-          const int col = pick_at(a, (base + t) * a.k + j);
-          if (col >= 0) tile[wave][of][col] = 0.0f;
-        }
-      wave_fence();
+      if constexpr (VALS) {
+        wave_fence();
+        picked([&](int c, float) { tile.put(c, 0.0f); });
+        wave_fence();
+      }
     }
   }
 }

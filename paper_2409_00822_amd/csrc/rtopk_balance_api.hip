@@ -71,10 +71,14 @@ int rtopk_balance_loss(const void* logits, int32_t dtype, int64_t N, int32_t E, 
   a.rows = l.rows;
   a.per_group = l.per_group;
   const int64_t parts = (int64_t)groups * l.per_group;
-  a.part_p = static_cast<double*>(workspace);
-  a.part_z = a.part_p + parts * E;
-  a.part_n = reinterpret_cast<int32_t*>(a.part_z + parts);
-  a.part_rows = a.part_n + parts * E;
+  if (l.per_group > 1) {
+    const int64_t blocks = (E + rtopk::kJoinCols - 1) / rtopk::kJoinCols;
+    a.part_p = static_cast<double*>(workspace);
+    a.part_z = reinterpret_cast<rtopk::BalancePart*>(a.part_p + parts * E);
+    a.part_dot = reinterpret_cast<double*>(a.part_z + parts);
+    a.part_n = reinterpret_cast<int32_t*>(a.part_dot + groups * blocks);
+    a.arrived = a.part_n + parts * E;
+  }
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err = rtopk::launch_balance(dtype, a, s);
   if (err == hipSuccess && l.per_group > 1) err = rtopk::launch_balance_join(a, s);

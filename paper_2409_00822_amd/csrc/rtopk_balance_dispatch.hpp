@@ -19,8 +19,11 @@ struct BalanceArgs {
   int col_bytes;
   float *loss, *z, *probs;  // [groups], [groups], [groups][E]
   int32_t *counts, *counted;  // [groups][E], [groups]
-  double *part_p, *part_z;  // [groups][per_group][E], [groups][per_group]
-  int32_t *part_n, *part_rows;
+  double* part_p;       // [groups][per_group][E]
+  BalancePart* part_z;  // [groups][per_group]
+  double* part_dot;     // [groups][blocks of columns]
+  int32_t* part_n;      // [groups][per_group][E]
+  int32_t* arrived;     // [groups]
   // gradient
   const float *grad_loss, *grad_z, *grad_vals;  // [groups], [groups] or null, [groups * per][k] or null
   const int32_t *counts_in, *counted_in;

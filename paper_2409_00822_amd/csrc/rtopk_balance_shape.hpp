@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include "rtopk_logits_shape.hpp"
+
 namespace rtopk {
 
 constexpr int kMaxExperts = 1024;
@@ -16,9 +18,11 @@ struct RouterLanes {
 };
 // X(lanes, loads)
 #define RTOPK_ROUTER_LIST(X) X(1, 1) X(2, 1) X(4, 1) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 4)
+constexpr bool is_router_of(int dtype, int loads) { return dtype == 0 || loads <= 2; }
+
 
 inline RouterLanes router_lanes(int E, int dtype) {
-  const int v = dtype == 0 ? 4 : 8, chunks = (E + v - 1) / v;
+  const int v = logits_width(dtype), chunks = (E + v - 1) / v;
 #define X(n, l) \
   if (chunks <= n * l) return {n, l};
   RTOPK_ROUTER_LIST(X)
@@ -42,9 +46,20 @@ inline BalanceLayout balance_layout(int64_t groups, int64_t per, int E, int dtyp
   return {rows, (int)((per + rows - 1) / rows)};
 }
 
-// Device memory for the workgroups' partial results: 64-bit sums of probabilities and of squared log-sum-exps, picks, tokens.
+constexpr int kJoinCols = 32;  // columns that a workgroup joins, all of them where there are
+constexpr int kFewParts = 32;  // or fewer parts to join
+
+// A workgroup's sum of squared log-sum-exps, tokens that count, picks.
+struct BalancePart {
+  double z;
+  int32_t counted, picked;
+};
+
+// Device memory for the workgroups' partial results: 64-bit sums of probabilities, the above, what blocks of columns have for a loss, picks, counters.
 inline int64_t balance_workspace(int64_t groups, int E, const BalanceLayout& l) {
-  return l.per_group > 1 ? groups * l.per_group * (8 * ((int64_t)E + 1) + 8 * (((int64_t)E + 2) / 2)) : 0;
+  if (l.per_group <= 1) return 0;
+  const int64_t parts = groups * l.per_group, blocks = (E + kJoinCols - 1) / kJoinCols;
+  return 8 * parts * E + 16 * parts + 8 * groups * blocks + 4 * parts * E + 4 * groups;
 }
 
 }  // namespace rtopk
