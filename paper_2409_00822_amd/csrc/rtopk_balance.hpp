@@ -70,19 +70,19 @@ struct RouterLane {
       for (int c = 0; c < V; ++c) keep[i][c] = !RAGGED || (has[i] && at[i] + c >= c0 && at[i] + c < E) ? 1.0f : 0.0f;
     }
   }
-  __device__ __forceinline__ void load(const elem* row, int E, u4_vec (&w)[LOADS]) const {
+  // -inf where the lane has nothing, or there is no such token
+  __device__ __forceinline__ void load(const elem* row, int E, bool is, u4_vec (&w)[LOADS]) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) w[i] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
     if (!RAGGED || E >= V) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        w[i] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
-        if (has[i]) w[i] = L::load_once(row + at[i]);
-      }
+      for (int i = 0; i < LOADS; ++i)
+        if (is && has[i]) w[i] = L::load_once(row + at[i]);
     } else {
       typename L::elem v[V];
+      if (is && has[0]) {
 #pragma unroll
-      for (int c = 0; c < V; ++c) v[c] = row[c < E ? c : 0];
-      w[0] = u4_vec{L::kLow, L::kLow, L::kLow, L::kLow};
-      if (has[0]) {
+        for (int c = 0; c < V; ++c) v[c] = row[c < E ? c : 0];
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           if constexpr (DT == kF32) w[0][c] = c < E ? __float_as_uint(v[c]) : L::kLow;
@@ -132,6 +132,13 @@ struct RouterRow {
       }
     s = lanes_sum<N>(s);
   }
+  __device__ __forceinline__ void clear() {  // for padding, which may hold NaN
+    m = s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+      for (int c = 0; c < V; ++c) e[i][c] = 0.0f;
+  }
 };
 
 // 1 / s of a sum of powers about the maximum (1 <= s <= kMaxExperts, or 0, or NaN), and the log-sum-exp, 0 for a row of nothing but -inf.
@@ -142,10 +149,11 @@ __device__ __forceinline__ float lse_of(float m, float s) {
   return s == 0.0f ? 0.0f : v;
 }
 
-__device__ __forceinline__ int pick_at(const BalanceArgs& a, int64_t i) {  // -1: none
-  const int c = a.col_bytes == 1 ? static_cast<const uint8_t*>(a.cols)[i] : static_cast<const int32_t*>(a.cols)[i];
+__device__ __forceinline__ int pick_from(const BalanceArgs& a, const char* p) {  // -1: none
+  const int c = a.col_bytes == 1 ? (int)*reinterpret_cast<const uint8_t*>(p) : *reinterpret_cast<const int32_t*>(p);
   return (uint32_t)c < (uint32_t)a.E ? c : -1;
 }
+__device__ __forceinline__ int pick_at(const BalanceArgs& a, int64_t i) { return pick_from(a, static_cast<const char*>(a.cols) + i * a.col_bytes); }
 
 // Whether a token of the lane's row has any pick: `any` of its N lanes, given their ballot.
 template <int N>
@@ -223,31 +231,34 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
         p[i][c] = 0.0f;
       }
   };
-  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U) {
+  const int64_t t1 = first + wave * (PER * U) + of;  // the lane's first token
+  const auto* px = x + t1 * a.stride;
+  const char* pc = static_cast<const char*>(a.cols) + ((base + t1) * a.k + sub) * a.col_bytes;
+  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U, px += W * PER * U * a.stride, pc += W * PER * U * a.k * a.col_bytes) {
+    const int left = (int)(end - t0);
     u4_vec w[U][LOADS];
     int col[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * PER + of, in = t < end ? t : end - 1;
-      r.load(x + in * a.stride, a.E, w[u]);
-      col[u] = sub < a.k && t < end ? pick_at(a, (base + in) * a.k + sub) : -1;
+      const bool is = u * PER + of < left;
+      r.load(px + u * PER * a.stride, a.E, is, w[u]);
+      col[u] = -1;
+      if (is && sub < a.k) col[u] = pick_from(a, pc + u * PER * a.k * a.col_bytes);
     }
     float own_m = 0.0f, own_s = 0.0f;  // of the token whose number is the lane's
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * PER + of;
-      if (t - of >= end) break;  // (uniform)
-      bool any = col[u] >= 0;
+      if (u * PER >= left) break;  // (uniform)
+      const bool any = col[u] >= 0;
       uint64_t ballot = __ballot(any);
       if (any) atomicAdd(&picks[col[u]], 1);
       picked += __popcll(ballot);
       RouterRow<DT, N, LOADS, RAGGED> row(r, w[u]);
-      float over = over_of(row.s);
       if (ballot == full && a.k <= N) {
         counted += PER;
       } else {
-        for (int j = sub + N; j - sub < a.k; j += N) {
-          const int more = j < a.k && t < end ? pick_at(a, (base + t) * a.k + j) : -1;
+        for (int j = N; j < a.k; j += N) {
+          const int more = sub + j < a.k && u * PER + of < left ? pick_from(a, pc + (u * PER * a.k + j) * a.col_bytes) : -1;
           if (more >= 0) atomicAdd(&picks[more], 1);
           const uint64_t b = __ballot(more >= 0);
           picked += __popcll(b);
@@ -255,14 +266,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
         }
         const bool counts = any_lane<N>(ballot, of);
         counted += __popcll(__ballot(counts && sub == 0));
-        if (!counts) {  // (padding may hold NaN)
-          row.s = row.m = over = 0.0f;
-#pragma unroll
-          for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-            for (int c = 0; c < V; ++c) row.e[i][c] = 0.0f;
-        }
+        if (!counts) row.clear();
       }
+      const float over = over_of(row.s);
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
 #pragma unroll
@@ -465,67 +471,80 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       const int e = r.at[i] + c;
-      w[i][c] = e < a.E ? (float)(each * a.counts_in[(int64_t)g * a.E + e]) : 0.0f;
+      w[i][c] = (float)a.counts_in[(int64_t)g * a.E + min(e, a.E - 1)];  // (no branch: together)
     }
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+    for (int c = 0; c < V; ++c) w[i][c] *= (float)each;
   const Tile tile{tiles[VALS ? wave : 0], a.E, of};
   if constexpr (VALS) {
     for (int c = lane; c < PER * V / 4 * Tile::PLANE; c += 64) (&tiles[wave][0][0][0])[c] = 0.0f;
     wave_fence();
   }
-  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U) {
+  const int64_t t1 = first + wave * (PER * U) + of;  // the lane's first token
+  const auto* px = x + t1 * a.stride;
+  auto* to = out + t1 * a.grad_stride;
+  const char* pc = static_cast<const char*>(a.cols) + ((base + t1) * a.k + sub) * a.col_bytes;
+  const float* pv = a.grad_vals + (VALS ? (base + t1) * a.k + sub : 0);
+  for (int64_t t0 = first + wave * (PER * U); t0 < end;
+       t0 += W * PER * U, px += W * PER * U * a.stride, to += W * PER * U * a.grad_stride, pc += W * PER * U * a.k * a.col_bytes, pv += VALS ? W * PER * U * a.k : 0) {
+    const int left = (int)(end - t0);
     u4_vec raw[U][LOADS];
     int col[U];
     float val[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * PER + of, in = t < end ? t : end - 1;
-      r.load(x + in * a.stride, a.E, raw[u]);
+      const bool is = u * PER + of < left;
+      r.load(px + u * PER * a.stride, a.E, is, raw[u]);
       col[u] = -1;
-      if (sub < a.k && t < end) {
-        col[u] = pick_at(a, (base + in) * a.k + sub);
-        if (VALS) val[u] = a.grad_vals[(base + in) * a.k + sub];
+      if (is && sub < a.k) {
+        col[u] = pick_from(a, pc + u * PER * a.k * a.col_bytes);
+        if (VALS) val[u] = pv[u * PER * a.k];
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * PER + of, entry = (base + t) * a.k;
-      if (t - of >= end) break;  // (uniform)
+      if (u * PER >= left) break;  // (uniform)
+      const bool is = u * PER + of < left;
+      const char* entry = pc + u * PER * a.k * a.col_bytes;
+      const float* value = pv + (VALS ? u * PER * a.k : 0);
       uint64_t ballot = __ballot(col[u] >= 0);
-      bool counts = true, once = true;  // once: picks that ascend, so that none is there twice
+      bool once = true;  // picks that ascend, so that none is there twice
       if (VALS) {
         const int before = __builtin_amdgcn_update_dpp(0, col[u], 0x138, 0xf, 0xf, false);  // wave_shr:1
         once = !__any(col[u] >= 0 && sub > 0 && !(before >= 0 && before < col[u]));
       }
+      RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
       if (!(ballot == full && a.k <= N)) {
-        for (int j = sub + N; j - sub < a.k; j += N) {
-          const int mine = j < a.k && t < end ? pick_at(a, entry + j) : -1;
+        for (int j = N; j < a.k; j += N) {
+          const int mine = sub + j < a.k && is ? pick_from(a, entry + j * a.col_bytes) : -1;
           ballot |= __ballot(mine >= 0);
           if (VALS) {
-            const int before = mine >= 0 ? pick_at(a, entry + j - 1) : -1;
+            const int before = mine >= 0 ? pick_from(a, entry + (j - 1) * a.col_bytes) : -1;
             once = once && !__any(mine >= 0 && !(before >= 0 && before < mine));
           }
         }
-        counts = any_lane<N>(ballot, of);
+        if (!any_lane<N>(ballot, of)) row.clear();
       }
       // f(column, the gradients that it gets) for the picks of the lane
       const auto picked = [&](auto f) {
         if (once) {
           if (col[u] >= 0) f(col[u], val[u]);
-          if (a.k > N && t < end)
-            for (int j = sub + N; j < a.k; j += N) {
-              const int mine = pick_at(a, entry + j);
-              if (mine >= 0) f(mine, a.grad_vals[entry + j]);
-            }
-        } else if (t < end) {
+          for (int j = N; j < a.k; j += N) {
+            const int mine = sub + j < a.k && is ? pick_from(a, entry + j * a.col_bytes) : -1;
+            if (mine >= 0) f(mine, value[j]);
+          }
+        } else if (is) {
           for (int j = sub; j < a.k; j += N) {
-            const int mine = pick_at(a, entry + j);
+            const int mine = pick_from(a, entry + (j - sub) * a.col_bytes);
             if (mine < 0) continue;
-            float v = a.grad_vals[entry + j];  // the first entry of a column adds up all that have it
+            float v = value[j - sub];  // the first entry of a column adds up all that have it
             bool earlier = false;
             for (int i = 0; i < a.k; ++i)
-              if (i != j && pick_at(a, entry + i) == mine) {
+              if (i != j && pick_from(a, entry + (i - sub) * a.col_bytes) == mine) {
                 earlier |= i < j;
-                v += a.grad_vals[entry + i];
+                v += value[i - sub];
               }
             if (!earlier) f(mine, v);
           }
@@ -535,7 +554,6 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
         picked([&](int c, float v) { tile.put(c, v); });
         wave_fence();
       }
-      const RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
       const float over = over_of(row.s);
       float dot = 0.0f;
 #pragma unroll
@@ -544,7 +562,6 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
         for (int c = 0; c < V; ++c) dot = __builtin_fmaf(r.kept(row.e[i][c], i, c), w[i][c], dot);
       dot = lanes_sum<N>(dot) * over;
       const float both = ((z2 == 0.0f ? 0.0f : z2 * lse_of(row.m, row.s)) - dot) * over;
-      auto* to = out + t * a.grad_stride;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         float d[V], v[V];
@@ -552,16 +569,16 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           d[c] = row.e[i][c] * __builtin_fmaf(w[i][c], over, both);
-          if (!counts) d[c] = 0.0f;
           if (VALS) d[c] += v[c];
         }
-        if (t < end && r.has[i]) {
+        if (is && r.has[i]) {
+          auto* at = to + u * PER * a.grad_stride + r.at[i];
           if (!RAGGED || a.E >= V) {
-            L::store(to + r.at[i], L::pack(d));
+            L::store(at, L::pack(d));
           } else {
 #pragma unroll
             for (int c = 0; c < V; ++c)
-              if (c < a.E) to[c] = L::narrow(d[c]);
+              if (c < a.E) at[c] = L::narrow(d[c]);
           }
         }
       }
