@@ -22,31 +22,40 @@ namespace rtopk {
 constexpr int kFlush = 64;  // tokens of a lane that fp32 sums run over
 constexpr float kFarMaximum = 1024.0f;  // log2(e) times a maximum beyond this is too coarse a reference: differences from the maximum are taken first
 
-// f over each N lanes (a power of two), the same in all of them.
-template <int N, typename F>
-__device__ __forceinline__ float lanes_reduce(float v, F f) {
-  const auto dpp = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
-  if constexpr (N >= 2) v = f(v, dpp(std::integral_constant<int, 0xb1>{}));   // quad_perm [1, 0, 3, 2]
-  if constexpr (N >= 4) v = f(v, dpp(std::integral_constant<int, 0x4e>{}));   // quad_perm [2, 3, 0, 1]
-  if constexpr (N >= 8) v = f(v, dpp(std::integral_constant<int, 0x141>{}));  // row_half_mirror
-  if constexpr (N >= 16) v = f(v, dpp(std::integral_constant<int, 0x140>{})); // row_mirror
+// Over each N lanes (a power of two), the same in all of them: within 16 lanes by DPP permutations that are part of the maximum or sum, then by swaps of rows.
+// (The maximum in assembly: a C++ one first quiets what might be a signalling NaN.)
+template <int N>
+__device__ __forceinline__ float lanes_max(float v) {
+  if constexpr (N >= 2) asm("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf" : "+v"(v));
+  if constexpr (N >= 4) asm("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf" : "+v"(v));
+  if constexpr (N >= 8) asm("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_half_mirror row_mask:0xf bank_mask:0xf" : "+v"(v));
+  if constexpr (N >= 16) asm("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_mirror row_mask:0xf bank_mask:0xf" : "+v"(v));
   if constexpr (N >= 32) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    v = vmax(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
   if constexpr (N >= 64) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    v = vmax(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
   return v;
 }
 template <int N>
-__device__ __forceinline__ float lanes_max(float v) {
-  return lanes_reduce<N>(v, [](float a, float b) { return fmaxf(a, b); });
-}
-template <int N>
 __device__ __forceinline__ float lanes_sum(float v) {
-  return lanes_reduce<N>(v, [](float a, float b) { return a + b; });
+  const auto dpp = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  if constexpr (N >= 2) v += dpp(std::integral_constant<int, 0xb1>{});   // quad_perm [1, 0, 3, 2]
+  if constexpr (N >= 4) v += dpp(std::integral_constant<int, 0x4e>{});   // quad_perm [2, 3, 0, 1]
+  if constexpr (N >= 8) v += dpp(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (N >= 16) v += dpp(std::integral_constant<int, 0x140>{}); // row_mirror
+  if constexpr (N >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (N >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
 }
 
 // The columns of a token's row that a lane has: chunk i of the lane is chunk `sub + i N` of the row.  RAGGED: the row is no whole number of chunks; its last chunk is
@@ -92,6 +101,12 @@ struct RouterLane {
       }
     }
   }
+  static __device__ __forceinline__ void leave_out(bool is, u4_vec (&w)[LOADS]) {  // (padding may hold NaN)
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) w[i][h] = is ? L::kLow : w[i][h];
+  }
   __device__ __forceinline__ float kept(float v, int i, int c) const { return RAGGED ? v * keep[i][c] : v; }
 };
 
@@ -132,13 +147,6 @@ struct RouterRow {
       }
     s = lanes_sum<N>(s);
   }
-  __device__ __forceinline__ void clear() {  // for padding, which may hold NaN
-    m = s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-      for (int c = 0; c < V; ++c) e[i][c] = 0.0f;
-  }
 };
 
 // 1 / s of a sum of powers about the maximum (1 <= s <= kMaxExperts, or 0, or NaN), and the log-sum-exp, 0 for a row of nothing but -inf.
@@ -149,11 +157,12 @@ __device__ __forceinline__ float lse_of(float m, float s) {
   return s == 0.0f ? 0.0f : v;
 }
 
-__device__ __forceinline__ int pick_from(const BalanceArgs& a, const char* p) {  // -1: none
-  const int c = a.col_bytes == 1 ? (int)*reinterpret_cast<const uint8_t*>(p) : *reinterpret_cast<const int32_t*>(p);
-  return (uint32_t)c < (uint32_t)a.E ? c : -1;
+// A column as it is stored, and whether it is a pick: looked at apart, so that a load is not waited for before the next one.
+__device__ __forceinline__ int stored_col(const BalanceArgs& a, const char* p) {
+  return a.col_bytes == 1 ? (int)*reinterpret_cast<const uint8_t*>(p) : *reinterpret_cast<const int32_t*>(p);
 }
-__device__ __forceinline__ int pick_at(const BalanceArgs& a, int64_t i) { return pick_from(a, static_cast<const char*>(a.cols) + i * a.col_bytes); }
+__device__ __forceinline__ int pick_of(const BalanceArgs& a, int col) { return (uint32_t)col < (uint32_t)a.E ? col : -1; }  // -1: none
+__device__ __forceinline__ int pick_from(const BalanceArgs& a, const char* p) { return pick_of(a, stored_col(a, p)); }
 
 // Whether a token of the lane's row has any pick: `any` of its N lanes, given their ballot.
 template <int N>
@@ -243,17 +252,16 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
       const bool is = u * PER + of < left;
       r.load(px + u * PER * a.stride, a.E, is, w[u]);
       col[u] = -1;
-      if (is && sub < a.k) col[u] = pick_from(a, pc + u * PER * a.k * a.col_bytes);
+      if (is && sub < a.k) col[u] = stored_col(a, pc + u * PER * a.k * a.col_bytes);
     }
     float own_m = 0.0f, own_s = 0.0f;  // of the token whose number is the lane's
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u * PER >= left) break;  // (uniform)
-      const bool any = col[u] >= 0;
+      const bool any = (uint32_t)col[u] < (uint32_t)a.E;
       uint64_t ballot = __ballot(any);
       if (any) atomicAdd(&picks[col[u]], 1);
       picked += __popcll(ballot);
-      RouterRow<DT, N, LOADS, RAGGED> row(r, w[u]);
       if (ballot == full && a.k <= N) {
         counted += PER;
       } else {
@@ -266,8 +274,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
         }
         const bool counts = any_lane<N>(ballot, of);
         counted += __popcll(__ballot(counts && sub == 0));
-        if (!counts) row.clear();
+        R::leave_out(!counts, w[u]);
       }
+      const RouterRow<DT, N, LOADS, RAGGED> row(r, w[u]);
       const float over = over_of(row.s);
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
@@ -499,7 +508,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
       r.load(px + u * PER * a.stride, a.E, is, raw[u]);
       col[u] = -1;
       if (is && sub < a.k) {
-        col[u] = pick_from(a, pc + u * PER * a.k * a.col_bytes);
+        col[u] = stored_col(a, pc + u * PER * a.k * a.col_bytes);
         if (VALS) val[u] = pv[u * PER * a.k];
       }
     }
@@ -509,13 +518,13 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
       const bool is = u * PER + of < left;
       const char* entry = pc + u * PER * a.k * a.col_bytes;
       const float* value = pv + (VALS ? u * PER * a.k : 0);
+      col[u] = pick_of(a, col[u]);
       uint64_t ballot = __ballot(col[u] >= 0);
       bool once = true;  // picks that ascend, so that none is there twice
       if (VALS) {
         const int before = __builtin_amdgcn_update_dpp(0, col[u], 0x138, 0xf, 0xf, false);  // wave_shr:1
         once = !__any(col[u] >= 0 && sub > 0 && !(before >= 0 && before < col[u]));
       }
-      RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
       if (!(ballot == full && a.k <= N)) {
         for (int j = N; j < a.k; j += N) {
           const int mine = sub + j < a.k && is ? pick_from(a, entry + j * a.col_bytes) : -1;
@@ -525,8 +534,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
             once = once && !__any(mine >= 0 && !(before >= 0 && before < mine));
           }
         }
-        if (!any_lane<N>(ballot, of)) row.clear();
+        R::leave_out(!any_lane<N>(ballot, of), raw[u]);
       }
+      const RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
       // f(column, the gradients that it gets) for the picks of the lane
       const auto picked = [&](auto f) {
         if (once) {
