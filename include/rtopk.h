@@ -333,7 +333,7 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
  *   out_rows   : [groups] int32_t, n.
  *   workspace  : as above, rtopk_balance_workspace_bytes(...) bytes.
  */
-int64_t rtopk_balance_workspace_bytes(int64_t N, int32_t E, int32_t dtype, int32_t groups);
+int64_t rtopk_balance_workspace_bytes(int64_t N, int32_t E, int32_t dtype, int32_t k, int32_t groups);
 int rtopk_balance_loss(const void* logits, int32_t dtype, int64_t N, int32_t E, int64_t stride, const void* cols, int32_t col_bytes, int32_t k,
                        int32_t groups, float* out_loss, float* out_z, float* out_probs, int32_t* out_counts, int32_t* out_rows, void* workspace,
                        int64_t workspace_bytes, void* stream);

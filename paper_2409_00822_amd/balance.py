@@ -9,9 +9,9 @@ from . import rtopk as _r
 from .logits import _given, _gradient, _output, _rows, _type
 
 
-def rtopk_balance_workspace_bytes(N: int, E: int, dtype, groups: int = 1) -> int:
-    """Device memory that the C entry point can use for such a call; dtype: of the logits."""
-    return int(_r.load_library().rtopk_balance_workspace_bytes(N, E, _type(dtype), groups))
+def rtopk_balance_workspace_bytes(N: int, E: int, dtype, k: int, groups: int = 1) -> int:
+    """Device memory that the C entry point can use for such a call; dtype: of the logits, k: picks of a token."""
+    return int(_r.load_library().rtopk_balance_workspace_bytes(N, E, _type(dtype), k, groups))
 
 
 def _picks(cols, N: int, groups: int, device):
@@ -43,7 +43,7 @@ def rtopk_balance_loss(logits, cols, groups: int = 1, out_loss=None, out_z=None,
     probs = _output(out_probs, torch.float32, (groups, E), device, "out_probs")
     counts = _output(out_counts, torch.int32, (groups, E), device, "out_counts")
     rows = _output(out_rows, torch.int32, (groups,), device, "out_rows")
-    n = rtopk_balance_workspace_bytes(N, E, logits.dtype, groups)
+    n = rtopk_balance_workspace_bytes(N, E, logits.dtype, cols.shape[1], groups)
     ws = torch.empty((n,), dtype=torch.uint8, device=device) if n > 0 else None
     with torch.cuda.device(device):
         _r._check(_r.load_library().rtopk_balance_loss(*x, *picks, loss.data_ptr(), z.data_ptr(), probs.data_ptr(), counts.data_ptr(), rows.data_ptr(),

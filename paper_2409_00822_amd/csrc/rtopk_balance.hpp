@@ -58,6 +58,25 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// Over the lanes that have the same place among their N, the same in all of them.
+template <int N>
+__device__ __forceinline__ float places_sum(float v) {
+  const auto ror = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + decltype(ctrl)::value, 0xf, 0xf, true)); };
+  if constexpr (N <= 1) v += ror(std::integral_constant<int, 1>{});
+  if constexpr (N <= 2) v += ror(std::integral_constant<int, 2>{});
+  if constexpr (N <= 4) v += ror(std::integral_constant<int, 4>{});
+  if constexpr (N <= 8) v += ror(std::integral_constant<int, 8>{});
+  if constexpr (N <= 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (N <= 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+
 // The columns of a token's row that a lane has: chunk i of the lane is chunk `sub + i N` of the row.  RAGGED: the row is no whole number of chunks; its last chunk is
 // moved back to end with it, and what that shares with the chunk before is held twice and counts once (`keep`).  Rows narrower than a chunk are loaded
 // by the element.
@@ -180,6 +199,31 @@ __device__ __forceinline__ uint64_t full_ballot(int k) {
   return all;
 }
 
+// A batch's loads are waited for once, here: a wait further on would also be one for the stores that have been made since.
+template <int U, int LOADS>
+__device__ __forceinline__ void arrived(u4_vec (&w)[U][LOADS], int (&col)[U]) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    apart(w[u]);
+    asm volatile("" : "+v"(col[u]));
+  }
+}
+
+// To nearest even, two values by one instruction where there is one.
+template <int DT>
+__device__ __forceinline__ u4_vec pack_rounded(const float (&v)[Logits<DT>::V]) {
+  if constexpr (DT == kBF16) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    u4_vec w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{v[2 * i], v[2 * i + 1]}), b2));
+    return w;
+  } else {
+    return Logits<DT>::pack(v);
+  }
+}
+
 // Loads of a lane that are made together.
 constexpr int balance_batch(int loads) { return loads == 1 ? 4 : (loads == 2 ? 2 : 1); }
 
@@ -215,13 +259,6 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % N, of = lane / N;
   const int g = blockIdx.x / a.per_group, part = blockIdx.x % a.per_group;
   const int64_t first = part * a.rows, end = first + a.rows < a.per ? first + a.rows : a.per, base = (int64_t)g * a.per;
-  for (int e = threadIdx.x; e < COLS; e += T) {
-    picks[e] = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) sums[w][e] = 0.0;
-  }
-  if (part == 0 && threadIdx.x == 0 && a.arrived) a.arrived[g] = 0;
-  __syncthreads();
   const auto* x = static_cast<const typename R::elem*>(a.x) + base * a.stride;
   const R r(a.E, sub);
   const uint64_t full = full_ballot<N>(a.k);
@@ -233,9 +270,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
     for (int i = 0; i < LOADS; ++i)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        float v = p[i][c];
-#pragma unroll
-        for (int d = N; d < 64; d <<= 1) v += __shfl_xor(v, d);
+        const float v = places_sum<N>(p[i][c]);
         if (of == 0 && r.has[i] && (!RAGGED || r.keep[i][c] != 0.0f)) sums[wave][r.at[i] + c] += v;
         p[i][c] = 0.0f;
       }
@@ -243,10 +278,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
   const int64_t t1 = first + wave * (PER * U) + of;  // the lane's first token
   const auto* px = x + t1 * a.stride;
   const char* pc = static_cast<const char*>(a.cols) + ((base + t1) * a.k + sub) * a.col_bytes;
-  for (int64_t t0 = first + wave * (PER * U); t0 < end; t0 += W * PER * U, px += W * PER * U * a.stride, pc += W * PER * U * a.k * a.col_bytes) {
-    const int left = (int)(end - t0);
-    u4_vec w[U][LOADS];
-    int col[U];
+  u4_vec w[U][LOADS];
+  int col[U];
+  const auto load = [&](int64_t left) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool is = u * PER + of < left;
@@ -254,6 +288,18 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_kernel(BalanceArgs
       col[u] = -1;
       if (is && sub < a.k) col[u] = stored_col(a, pc + u * PER * a.k * a.col_bytes);
     }
+  };
+  int64_t left = end - first - wave * (PER * U);
+  load(left);  // (before all else: the first batch comes meanwhile)
+  for (int e = threadIdx.x; e < COLS; e += T) {
+    picks[e] = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) sums[w][e] = 0.0;
+  }
+  if (part == 0 && threadIdx.x == 0 && a.arrived) a.arrived[g] = 0;
+  __syncthreads();
+  for (; left > 0; left -= W * PER * U, px += W * PER * U * a.stride, pc += W * PER * U * a.k * a.col_bytes, load(left)) {
+    arrived(w, col);
     float own_m = 0.0f, own_s = 0.0f;  // of the token whose number is the lane's
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -435,12 +481,21 @@ struct PickedTile {
   static constexpr int V = Logits<DT>::V, PER = 64 / N, PLANE = N * LOADS * 4;
   float (&at)[PER][V / 4][PLANE];
   int E, of;
-  __device__ __forceinline__ float& place(int chunk, int c) const { return at[of][c / 4][chunk * 4 + c % 4]; }
-  __device__ __forceinline__ void put(int col, float v) const {
-    const int last = (E - 1) / V;  // the chunk that ends with the row
-    if (!RAGGED || E < V || col / V != last) place(col / V, col % V) = v;
-    if (RAGGED && E >= V && col >= E - V) place(last, col - (E - V)) = v;
+  __device__ __forceinline__ float* place(int chunk, int c) const { return &at[of][c / 4][chunk * 4 + c % 4]; }
+  // where a column is held: for the lane that has it, and for the one whose chunk ends with the row
+  struct Places {
+    float *own, *end;
+    __device__ __forceinline__ void put(float v) const {
+      if (!RAGGED || own) *own = v;
+      if (RAGGED && end) *end = v;
+    }
+  };
+  __device__ __forceinline__ Places places(int col) const {
+    if (!RAGGED || E < V) return {place(col / V, col % V), nullptr};
+    const int last = (E - 1) / V;
+    return {col / V != last ? place(col / V, col % V) : nullptr, col >= E - V ? place(last, col - (E - V)) : nullptr};
   }
+  __device__ __forceinline__ void put(int col, float v) const { places(col).put(v); }
   __device__ __forceinline__ void get(int chunk, float (&v)[V]) const {
 #pragma unroll
     for (int h = 0; h < V / 4; ++h) {
@@ -467,6 +522,29 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
   auto* out = static_cast<typename L::elem*>(a.grad_x) + base * a.grad_stride;
   const R r(a.E, sub);
   const uint64_t full = full_ballot<N>(a.k);
+  const int64_t t1 = first + wave * (PER * U) + of;  // the lane's first token
+  const auto* px = x + t1 * a.stride;
+  auto* to = out + t1 * a.grad_stride;
+  const char* pc = static_cast<const char*>(a.cols) + ((base + t1) * a.k + sub) * a.col_bytes;
+  const float* pv = a.grad_vals + (VALS ? (base + t1) * a.k + sub : 0);
+  u4_vec raw[U][LOADS];
+  int col[U];
+  float val[U];
+  const auto load = [&](int64_t left) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool is = u * PER + of < left;
+      r.load(px + u * PER * a.stride, a.E, is, raw[u]);
+      col[u] = -1;
+      val[u] = 0.0f;
+      if (is && sub < a.k) {
+        col[u] = stored_col(a, pc + u * PER * a.k * a.col_bytes);
+        if (VALS) val[u] = pv[u * PER * a.k];
+      }
+    }
+  };
+  int64_t left = end - first - wave * (PER * U);
+  load(left);  // (before all else: the first batch comes meanwhile)
   // w_e of the lane's columns
   float w[LOADS][V];
   double all = 0.0;
@@ -491,26 +569,12 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
     for (int c = lane; c < PER * V / 4 * Tile::PLANE; c += 64) (&tiles[wave][0][0][0])[c] = 0.0f;
     wave_fence();
   }
-  const int64_t t1 = first + wave * (PER * U) + of;  // the lane's first token
-  const auto* px = x + t1 * a.stride;
-  auto* to = out + t1 * a.grad_stride;
-  const char* pc = static_cast<const char*>(a.cols) + ((base + t1) * a.k + sub) * a.col_bytes;
-  const float* pv = a.grad_vals + (VALS ? (base + t1) * a.k + sub : 0);
-  for (int64_t t0 = first + wave * (PER * U); t0 < end;
-       t0 += W * PER * U, px += W * PER * U * a.stride, to += W * PER * U * a.grad_stride, pc += W * PER * U * a.k * a.col_bytes, pv += VALS ? W * PER * U * a.k : 0) {
-    const int left = (int)(end - t0);
-    u4_vec raw[U][LOADS];
-    int col[U];
-    float val[U];
+  for (; left > 0; left -= W * PER * U, px += W * PER * U * a.stride, to += W * PER * U * a.grad_stride, pc += W * PER * U * a.k * a.col_bytes,
+                  pv += VALS ? W * PER * U * a.k : 0, load(left)) {
+    arrived(raw, col);
+    if (VALS) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool is = u * PER + of < left;
-      r.load(px + u * PER * a.stride, a.E, is, raw[u]);
-      col[u] = -1;
-      if (is && sub < a.k) {
-        col[u] = stored_col(a, pc + u * PER * a.k * a.col_bytes);
-        if (VALS) val[u] = pv[u * PER * a.k];
-      }
+      for (int u = 0; u < U; ++u) asm volatile("" : "+v"(val[u]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -537,10 +601,9 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
         R::leave_out(!any_lane<N>(ballot, of), raw[u]);
       }
       const RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
-      // f(column, the gradients that it gets) for the picks of the lane
+      // f(column, the gradients that it gets) for the picks of the lane, but for the first where there is one to a column
       const auto picked = [&](auto f) {
         if (once) {
-          if (col[u] >= 0) f(col[u], val[u]);
           for (int j = N; j < a.k; j += N) {
             const int mine = sub + j < a.k && is ? pick_from(a, entry + j * a.col_bytes) : -1;
             if (mine >= 0) f(mine, value[j]);
@@ -560,7 +623,13 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
           }
         }
       };
+      typename Tile::Places own = {};
+      const bool first_pick = VALS && once && col[u] >= 0;
       if constexpr (VALS) {
+        if (first_pick) {
+          own = tile.places(col[u]);
+          own.put(val[u]);
+        }
         picked([&](int c, float v) { tile.put(c, v); });
         wave_fence();
       }
@@ -578,13 +647,13 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
         if (VALS) tile.get(sub + i * N, v);
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          d[c] = row.e[i][c] * __builtin_fmaf(w[i][c], over, both);
-          if (VALS) d[c] += v[c];
+          const float t = __builtin_fmaf(w[i][c], over, both);
+          d[c] = VALS ? __builtin_fmaf(row.e[i][c], t, v[c]) : row.e[i][c] * t;
         }
         if (is && r.has[i]) {
           auto* at = to + u * PER * a.grad_stride + r.at[i];
           if (!RAGGED || a.E >= V) {
-            L::store(at, L::pack(d));
+            L::store(at, pack_rounded<DT>(d));
           } else {
 #pragma unroll
             for (int c = 0; c < V; ++c)
@@ -594,6 +663,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
       }
       if constexpr (VALS) {
         wave_fence();
+        if (first_pick) own.put(0.0f);
         picked([&](int c, float) { tile.put(c, 0.0f); });
         wave_fence();
       }

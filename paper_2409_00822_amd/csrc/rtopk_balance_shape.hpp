@@ -17,17 +17,17 @@ struct RouterLanes {
   int lanes, loads;
 };
 // X(lanes, loads)
-#define RTOPK_ROUTER_LIST(X) X(1, 1) X(2, 1) X(4, 1) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 4)
+#define RTOPK_ROUTER_LIST(X) \
+  X(1, 1) X(2, 1) X(4, 1) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(2, 2) X(4, 2) X(8, 2) X(16, 2) X(32, 2) X(64, 2) X(64, 4)
 constexpr bool is_router_of(int dtype, int loads) { return dtype == 0 || loads <= 2; }
 
-
-inline RouterLanes router_lanes(int E, int dtype) {
+// Two loads to a lane where a token's picks still have a lane each: what is done once for all columns of a lane is then done for half as many lanes.
+inline RouterLanes router_lanes(int E, int dtype, int k) {
   const int v = logits_width(dtype), chunks = (E + v - 1) / v;
-#define X(n, l) \
-  if (chunks <= n * l) return {n, l};
-  RTOPK_ROUTER_LIST(X)
-#undef X
-  return {0, 0};
+  int n = 1;
+  while (n < 64 && n < chunks) n *= 2;
+  if (chunks > 64) return {64, chunks <= 128 ? 2 : 4};
+  return n >= 4 && n / 2 >= k ? RouterLanes{n / 2, 2} : RouterLanes{n, 1};
 }
 
 // `per_group` workgroups to a group, `rows` tokens each (the last one what is left).
@@ -36,8 +36,8 @@ struct BalanceLayout {
   int per_group;
 };
 
-inline BalanceLayout balance_layout(int64_t groups, int64_t per, int E, int dtype, bool spread) {
-  const RouterLanes r = router_lanes(E, dtype);
+inline BalanceLayout balance_layout(int64_t groups, int64_t per, int E, int dtype, int k, bool spread) {
+  const RouterLanes r = router_lanes(E, dtype, k);
   const int64_t at_once = kBalanceWaves * (64 / r.lanes);  // tokens that a workgroup takes at a time
   if (!spread || per <= at_once) return {per, 1};
   int64_t n = (1024 + groups - 1) / groups, most = (per + at_once - 1) / at_once;

@@ -362,10 +362,10 @@ __device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, 
   return at;
 }
 
-// A draw by u from the weights of a row: rest[j] are its pieces' sums where they are p - q, else part[j] their masses in p.  Draws from p where the weights'
+// A draw by u from the weights of a row: rest(j) are its pieces' sums where they are p - q, else part[j] their masses in p.  Draws from p where the weights'
 // whole is no more than kLeastMass.
-template <int DT, int W>
-__device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, const double2* part, const double* rest, double u,
+template <int DT, int W, typename R>
+__device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, const double2* part, R rest, double u,
                           FindRoom<W>& room) {
   const int lane = threadIdx.x & 63;
   const auto cols = [&](int j) { return min(a.piece_cols, a.M - j * a.piece_cols); };
@@ -374,7 +374,7 @@ __device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT
   const double special_sum = special >= 0 ? piece_weight<DT>(w, p, q, special * a.piece_cols, cols(special), lane) : 0.0;
   for (;;) {
     const auto sum = [&](int j) {
-      if (w.less) return rest[j];
+      if (w.less) return rest(j);
       if (w.without >= 0 && j == special) return special_sum;
       const double2 t = part[j];
       return t.y * (t.x == w.p.ref || t.y == 0.0 ? 1.0 : power2((t.x - w.p.ref) * w.c)) * w.over_p;
@@ -510,7 +510,7 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
         });
         __syncthreads();
       }
-      drawn = block_draw<DT, W>(a, w, p, q, part, rest, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+      drawn = block_draw<DT, W>(a, w, p, q, part, [&](int j) { return rest[j]; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
     }
   }
   write_sequence(a, n, pos, drawn, 64 * W);
@@ -629,16 +629,16 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) 
     const int piece = group * W + wave, first = piece * a.piece_cols;
     if (piece < a.pieces) {
       const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
-      if (lane == 0) rest[piece] = s;
+      if (lane == 0) __hip_atomic_store(rest + piece, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.arrived + n, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)groups - 1;
+    __syncthreads();  // (the stores are done: they, and the loads of the last workgroup, go past the caches, which need not be written back then)
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.arrived + n, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)groups - 1;
     __syncthreads();
     if (!last) return;
-    __threadfence();
   }
-  const int drawn = block_draw<DT, W>(a, w, p, q, parts + (int64_t)pos * a.pieces, rest, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+  const int drawn = block_draw<DT, W>(
+      a, w, p, q, parts + (int64_t)pos * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
+      (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }
 

@@ -18,7 +18,7 @@ hipError_t grad_of(const BalanceArgs& a, hipStream_t s) {
 
 template <int DT>
 hipError_t grad_of_type(const BalanceArgs& a, hipStream_t s) {
-  const RouterLanes r = router_lanes(a.E, DT);
+  const RouterLanes r = router_lanes(a.E, DT, a.k);
 #define X(n, l)                      \
   if constexpr (is_router_of(DT, l)) \
     if (r.lanes == n && r.loads == l) return grad_of<DT, n, l>(a, s);

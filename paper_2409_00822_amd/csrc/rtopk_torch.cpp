@@ -711,7 +711,7 @@ PyObject* balance_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
     float *p_loss = floats(loss), *p_z = floats(z), *p_probs = floats(probs);
     int32_t *p_counts = static_cast<int32_t*>(counts.tensor.data_ptr()), *p_rows = static_cast<int32_t*>(rows.tensor.data_ptr());
     void* s = stream_of(*x);
-    Memory w(rtopk_balance_workspace_bytes(r.N, r.M, r.dtype, groups), device, plain);
+    Memory w(rtopk_balance_workspace_bytes(r.N, r.M, r.dtype, c.k, groups), device, plain);
     const c10::hip::HIPGuard on(device.index());
     const int status = unlocked([&] {
       return rtopk_balance_loss(r.data, r.dtype, r.N, r.M, r.stride, c.data, c.bytes, c.k, groups, p_loss, p_z, p_probs, p_counts, p_rows, w.data, w.bytes, s);

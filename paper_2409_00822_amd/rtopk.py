@@ -75,7 +75,7 @@ def load_library() -> ctypes.CDLL:
         draw = [vp, vp, ctypes.c_double]  # uniforms, temperatures, temperature
         lib.rtopk_sample_tokens.argtypes = [*rows, *draw, vp, i32, vp, i64, vp]
         lib.rtopk_verify_drafts.argtypes = [vp, vp, i32, i64, i32, i32, i64, i64, i64, i64, vp, i32, *draw, vp, vp, vp, i64, vp]
-        lib.rtopk_balance_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        lib.rtopk_balance_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
         lib.rtopk_balance_workspace_bytes.restype = i64
         picks = [vp, i32, i32, i32]  # cols, col_bytes, k, groups
         lib.rtopk_balance_loss.argtypes = [*rows, *picks, vp, vp, vp, vp, vp, vp, i64, vp]

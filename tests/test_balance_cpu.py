@@ -54,8 +54,8 @@ def test_refusals(lib):
 
 def test_scratch_memory(lib):
     f = lib.rtopk_balance_workspace_bytes
-    assert f(1 << 20, 64, BF16, 1) > 0 and f(16, 64, BF16, 1) == 0 and f(1 << 20, 64, BF16, 1 << 20) == 0
-    for bad in ((0, 64, F32, 1), (10, 0, F32, 1), (10, 1025, F32, 1), (10, 64, 5, 1), (10, 64, F32, 3), (10, 64, F32, 0)):
+    assert f(1 << 20, 64, BF16, 2, 1) > 0 and f(16, 64, BF16, 2, 1) == 0 and f(1 << 20, 64, BF16, 2, 1 << 20) == 0
+    for bad in ((0, 64, F32, 2, 1), (10, 0, F32, 2, 1), (10, 1025, F32, 2, 1), (10, 64, 5, 2, 1), (10, 64, F32, 0, 1), (10, 64, F32, 65, 1), (10, 64, F32, 2, 3), (10, 64, F32, 2, 0)):
         assert f(*bad) == 0
 
 
@@ -66,28 +66,32 @@ using namespace rtopk;
 int main() {
   long bad = 0, all = 0;
   const int64_t pers[] = {0, 1, 2, 3, 7, 31, 64, 65, 100, 1000, 4096, 99999, 1 << 20, (int64_t)1 << 30, ((int64_t)1 << 31) - 1};
+  const int ks[] = {1, 2, 3, 4, 6, 8, 12, 16, 33, 64, 1024};
   const int64_t counts[] = {1, 2, 3, 8, 100, 1000, 1024, 1025, 65536, 1 << 20};
   for (int dtype = 0; dtype < 3; ++dtype)
-    for (int E = 1; E <= kMaxExperts; ++E) {
-      const RouterLanes r = router_lanes(E, dtype);
-      const int v = dtype == 0 ? 4 : 8;
-      if (r.lanes < 1 || r.lanes > 64 || (r.lanes & (r.lanes - 1)) || r.lanes * r.loads * v < E) ++bad;
-      bool compiled = false;
-#define X(n, l) compiled |= r.lanes == n && r.loads == l;
-      RTOPK_ROUTER_LIST(X)
+    for (int E = 1; E <= kMaxExperts; ++E)
+      for (int k : ks) {
+        if (k > E) continue;
+        const RouterLanes r = router_lanes(E, dtype, k);
+        const int v = dtype == 0 ? 4 : 8;
+        if (r.lanes < 1 || r.lanes > 64 || (r.lanes & (r.lanes - 1)) || r.lanes * r.loads * v < E) ++bad;
+        if (E % v == 0 ? (r.lanes * r.loads - r.lanes) * v >= E && r.loads > 1 && r.lanes > 1 && r.lanes * v >= E : false) ++bad;  // no load that all lanes lack
+        bool compiled = false;
+#define X(n, l) compiled |= r.lanes == n && r.loads == l && is_router_of(dtype, l);
+        RTOPK_ROUTER_LIST(X)
 #undef X
-      if (!compiled) ++bad;
-      for (int64_t per : pers)
-        for (int64_t groups : counts)
-          for (int spread = 0; spread < 2; ++spread) {
-            const BalanceLayout l = balance_layout(groups, per, E, dtype, spread);
-            ++all;
-            // every token in one workgroup, none empty unless the group is
-            if (l.per_group < 1 || l.rows * l.per_group < per || (l.per_group > 1 && l.rows * (l.per_group - 1) >= per)) ++bad;
-            if (!spread && l.per_group != 1) ++bad;
-            if (groups * l.per_group > ((int64_t)1 << 23)) ++bad;  // 2^31 threads
-          }
-    }
+        if (!compiled) ++bad;
+        for (int64_t per : pers)
+          for (int64_t groups : counts)
+            for (int spread = 0; spread < 2; ++spread) {
+              const BalanceLayout l = balance_layout(groups, per, E, dtype, k, spread);
+              ++all;
+              // every token in one workgroup, none empty unless the group is
+              if (l.per_group < 1 || l.rows * l.per_group < per || (l.per_group > 1 && l.rows * (l.per_group - 1) >= per)) ++bad;
+              if (!spread && l.per_group != 1) ++bad;
+              if (groups * l.per_group > ((int64_t)1 << 23)) ++bad;  // 2^31 threads
+            }
+      }
   printf("%ld %ld\n", bad, all);
   return bad != 0;
 }
