@@ -234,7 +234,7 @@ struct Weights {
   bool less;    // p - q
   __device__ __forceinline__ double at(int col, float xp, float xq) const {
     const double v = p.power(xp, c) * over_p;
-    if (less) return fmax(v - q.power(xq, c) * over_q, 0.0);
+    if (less) return fmax(__builtin_fma(p.power(xp, c), over_p, -(q.power(xq, c) * over_q)), 0.0);
     return col == without ? 0.0 : v;
   }
   __device__ __forceinline__ bool is_number() const { return over_p == over_p && (!less || over_q == over_q); }
@@ -247,11 +247,21 @@ __device__ __forceinline__ void each_weight(const Weights& w, const typename Log
   const int full = cols / L::V, rest = cols % L::V;
   const auto *a = p + first, *b = (w.less ? q : p) + first;
   double v[L::V];
-  for (; i < full; i += T) {
-    const u4_vec x = L::load(a + (int64_t)i * L::V), y = w.less ? L::load(b + (int64_t)i * L::V) : x;
+  if (w.less && w.p.ref == 0.0 && w.q.ref == 0.0) {  // (mostly; neither row has a NaN or +inf)
+    const auto power = [&](float x) { return power2_finite((double)fmaxf(x, -3.402823466e38f) * w.c); };
+    for (; i < full; i += T) {
+      const u4_vec x = L::load(a + (int64_t)i * L::V), y = L::load(b + (int64_t)i * L::V);
 #pragma unroll
-    for (int c = 0; c < L::V; ++c) v[c] = w.at(first + i * L::V + c, L::at(x, c), L::at(y, c));
-    f(v, first + i * L::V);
+      for (int c = 0; c < L::V; ++c) v[c] = fmax(__builtin_fma(power(L::at(x, c)), w.over_p, -(power(L::at(y, c)) * w.over_q)), 0.0);
+      f(v, first + i * L::V);
+    }
+  } else {
+    for (; i < full; i += T) {
+      const u4_vec x = L::load(a + (int64_t)i * L::V), y = w.less ? L::load(b + (int64_t)i * L::V) : x;
+#pragma unroll
+      for (int c = 0; c < L::V; ++c) v[c] = w.at(first + i * L::V + c, L::at(x, c), L::at(y, c));
+      f(v, first + i * L::V);
+    }
   }
   if (i == full && rest != 0) {
 #pragma unroll
@@ -439,22 +449,21 @@ __device__ __forceinline__ const typename Logits<DT>::elem* row_of(const DrawArg
   return row <= a.G ? static_cast<const elem*>(a.target) + n * a.target_seq + row * a.target_pos
                     : static_cast<const elem*>(a.draft) + n * a.draft_seq + (row - a.G - 1) * a.draft_pos;
 }
-__device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.draft ? 2 * a.G + 1 : a.G + 1; }
 
 // One workgroup takes a sequence: its rows one after the other until a draft is rejected, then the draw.
 template <int DT, int W>
 __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
   using elem = typename Logits<DT>::elem;
   __shared__ FindRoom<W> room;
-  __shared__ double2 part[kMostPieces];
-  __shared__ double2 draft_part[kMostPieces];  // then the sums of p - q
+  __shared__ double2 part[kMostPieces], draft_part[kMostPieces];  // masses of pieces; then the sums of p - q in the latter's place
   const int64_t n = a.row0 + blockIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Heat heat(a, n);
+  int pos = 0;
   const auto each_piece = [&](auto f) {
     for (int j = wave; j < a.pieces; j += W) f(j, j * a.piece_cols, min(a.piece_cols, a.M - j * a.piece_cols));
   };
-  int pos = 0, drawn = -1;
+  int drawn = -1;
   if (heat.certain()) {
     for (;; ++pos) {
       const elem* x = row_of<DT>(a, n, pos);
@@ -516,23 +525,93 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
   write_sequence(a, n, pos, drawn, 64 * W);
 }
 
-// ---- few sequences, spread over workgroups ---------------------------------------------------------
+// ---- drafts tested beforehand ----------------------------------------------------------------------
 
-// The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  All rows that may be looked at, those
-// behind a rejected draft among them: their workgroups have the GPU to themselves otherwise.
+// fp32 sums of a row and the power at a draft are off by up to 64 units of 2^-24 each.  Where u q and p are nearer to each other than this part of them, they are
+// computed again in 64 bits.
+constexpr double kTestMargin = 0x1p-15;
+
+// The first of `most` positions whose draft the tests have rejected; each wavefront for itself.
+__device__ __forceinline__ int tested_up_to(const DrawArgs& a, int64_t n, int most) {
+  const int lane = threadIdx.x & 63;
+  for (int j = 0; j < most; j += 64) {
+    const uint64_t stop = __ballot(j + lane >= most || a.accepts[n * a.G + min(j + lane, most - 1)] == 0);
+    if (stop != 0) return j + __builtin_ctzll(stop);
+  }
+  return most;
+}
+
+// Tests positions [pos0, pos0 + positions) of the sequences whose drafts before that have been accepted, a workgroup to each: most rows are read once, in fp32, at
+// the rate of HBM, and those behind a rejected draft not at all.
+template <int DT, int W>
+__global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0, int positions) {
+  using elem = typename Logits<DT>::elem;
+  constexpr int T = 64 * W;
+  __shared__ float4 sums[W];
+  __shared__ double2 part[W];
+  const int64_t n = a.row0 + blockIdx.x / (uint32_t)positions;
+  const int pos = pos0 + (int)(blockIdx.x % (uint32_t)positions), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Heat heat(a, n);
+  if (heat.none() || pos >= drafts_of(a, n) || tested_up_to(a, n, pos0) < pos0) return;
+  const int d = draft_at(a, n, pos), cols = (a.M + W - 1) / W, first = min(wave * cols, a.M), mine = min(cols, a.M - first);
+  const elem *p = row_of<DT>(a, n, pos), *q = a.draft ? row_of<DT>(a, n, a.G + 1 + pos) : p;
+  bool accepted;
+  if (heat.certain()) {
+    const Best b = piece_best<DT>(p, first, mine, lane);
+    if (lane == 0) part[wave] = b.stored();
+    __syncthreads();
+    accepted = join_best(part, W).col() == d;
+  } else {
+    const double u = (double)a.uniforms[n * (a.G + 1) + pos];
+    const float c = (float)heat.c;
+    const auto near = [&](const elem* x) {
+      const Segment<DT> g(x, a.M);
+      const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, 4, false, false>(g, c), c, sums);
+      __syncthreads();
+      return power2(((double)Logits<DT>::widen(x[d]) - (double)t.m) * heat.c) / (double)t.s;
+    };
+    double p_d = near(p), uq = a.draft ? u * near(q) : u;
+    accepted = uq < p_d * (1.0 - kTestMargin);
+    if (!accepted && !(uq > p_d * (1.0 + kTestMargin))) {
+      const auto exact = [&](const elem* x) {
+        const Mass t = piece_mass<DT>(x + first, mine, lane, heat.c);
+        __syncthreads();
+        if (lane == 0) part[wave] = make_double2(t.ref, t.s);
+        __syncthreads();
+        const Mass all = join_mass(part, W, heat.c);
+        return all.power(Logits<DT>::widen(x[d]), heat.c) * all.over();
+      };
+      p_d = exact(p);
+      uq = a.draft ? u * exact(q) : u;
+      accepted = uq < p_d;
+    }
+  }
+  if (threadIdx.x == 0) a.accepts[n * a.G + pos] = accepted;
+}
+
+// ---- sequences spread over workgroups --------------------------------------------------------------
+
+// Rows of a sequence whose masses are kept: of all its positions, the target's first, or (tested) of the one that is drawn at.
+__device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.accepts ? (a.draft ? 2 : 1) : (a.draft ? 2 * a.G + 1 : a.G + 1); }
+
+// The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  Untested, all rows that may be looked at, those
+// behind a rejected draft among them: few sequences leave the GPU room for that.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) {
   const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves, of = blockIdx.x / groups, rows = (uint32_t)rows_of(a);
-  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, row = (int)(of % rows);
+  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, kept = (int)(of % rows);
   const int64_t n = a.row0 + of / rows;
-  if (a.arrived && blockIdx.x % groups == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
+  if (a.arrived && blockIdx.x % groups == 0 && kept == 0 && threadIdx.x == 0) a.arrived[n] = 0;
   if (piece >= a.pieces) return;
   const Heat heat(a, n);
-  if (heat.none() || (heat.certain() && row > a.G)) return;
+  int row = kept;
+  if (heat.none()) return;
   if (a.G > 0) {
     const int g = drafts_of(a, n);
+    if (a.accepts) row = tested_up_to(a, n, g) + (kept == 0 ? 0 : a.G + 1);
     if (row <= a.G ? row > g : row - a.G - 1 >= g) return;
   }
+  if (heat.certain() && row > a.G) return;
   const auto* x = row_of<DT>(a, n, row);
   const int first = piece * a.piece_cols, cols = min(a.piece_cols, a.M - first);
   double2 out;
@@ -542,20 +621,20 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) 
     const Mass t = piece_mass<DT>(x + first, cols, lane, heat.c);
     out = make_double2(t.ref, t.s);
   }
-  if (lane == 0) a.part[(n * rows + row) * a.pieces + piece] = out;
+  if (lane == 0) a.part[(n * rows + kept) * a.pieces + piece] = out;
 }
 
 // Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
 // last one of them that is done (counted from 0, which draw_mass_kernel set) goes on; else the first one does it alone.  Which one is last changes
 // nothing: sums lie in memory and are taken in order.
-template <int DT>
-__global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) {
+template <int DT, int W>
+__global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
   using elem = typename Logits<DT>::elem;
-  constexpr int W = kDrawWaves, T = 64 * W;
+  constexpr int T = 64 * W;
   __shared__ FindRoom<W> room;
   __shared__ double2 mass[2 * kMaxDrafts + 1];
   __shared__ int best[kMaxDrafts + 1], last;
-  const uint32_t groups = a.draft ? (uint32_t)(a.pieces + W - 1) / W : 1;
+  const uint32_t groups = (uint32_t)a.groups;
   const int group = (int)(blockIdx.x % groups), rows = rows_of(a);
   const int64_t n = a.row0 + blockIdx.x / groups;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -564,40 +643,53 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) 
     if (group == 0) write_sequence(a, n, 0, -1, T);
     return;
   }
-  const int g = a.G > 0 ? drafts_of(a, n) : 0;
+  const int g = a.G > 0 ? drafts_of(a, n) : 0, from = a.accepts ? tested_up_to(a, n, g) : 0, to = a.accepts ? from : g;  // positions whose masses there are
+  const auto kept = [&](int row) { return a.accepts ? (row <= a.G ? 0 : 1) : row; };
   const double2* parts = a.part + n * rows * a.pieces;
   if (heat.certain()) {
     if (group != 0) return;
-    for (int row = wave; row <= g; row += W) {
-      const int col = join_best(parts + row * a.pieces, a.pieces).col();
+    for (int row = from + wave; row <= to; row += W) {
+      const int col = join_best(parts + (int64_t)kept(row) * a.pieces, a.pieces).col();
       if (lane == 0) best[row] = col;
     }
     __syncthreads();
-    int pos = 0;
-    while (pos < g && best[pos] >= 0 && best[pos] == draft_at(a, n, pos)) ++pos;
+    int pos = from;
+    while (pos < to && best[pos] >= 0 && best[pos] == draft_at(a, n, pos)) ++pos;
     write_sequence(a, n, pos, best[pos], T);
     return;
   }
-  for (int i = wave; i < (a.draft ? 2 * g + 1 : g + 1); i += W) {
-    const int row = i <= g ? i : a.G + i - g;
-    const Mass t = join_mass(parts + (int64_t)row * a.pieces, a.pieces, heat.c);
+  // what the tests need, before the masses are there
+  float p_at = 0.0f, q_at = 0.0f, u = 0.0f;
+  const auto look = [&](int i) {
+    if (i < to) {
+      const int d = draft_at(a, n, i);
+      u = a.uniforms[n * (a.G + 1) + i];
+      p_at = Logits<DT>::widen(row_of<DT>(a, n, i)[d]);
+      if (a.draft) q_at = Logits<DT>::widen(row_of<DT>(a, n, a.G + 1 + i)[d]);
+    }
+  };
+  look(from + lane);
+  const int targets = to - from + 1, drafts = a.draft ? min(to + 1, g) - from : 0;
+  for (int i = wave; i < targets + drafts; i += W) {
+    const int row = i < targets ? from + i : a.G + 1 + from + i - targets;
+    const Mass t = join_mass(parts + (int64_t)kept(row) * a.pieces, a.pieces, heat.c);
     if (lane == 0) mass[row] = make_double2(t.ref, t.s);
   }
   __syncthreads();
   const auto mass_of = [&](int row) { return Mass{mass[row].x, mass[row].y}; };
-  int pos = g;  // the first rejected draft
-  for (int j = 0; j < g; j += 64) {
+  int pos = to;  // of the first rejected draft, or behind them all
+  for (int j = from; j < to; j += 64) {  // (untested)
     bool rejected = false;
     const int i = j + lane;
-    if (i < g) {
-      const int d = draft_at(a, n, i);
+    if (j > from) look(i);
+    if (i < to) {
       const Mass p = mass_of(i);
       double q_d = 1.0;
       if (a.draft) {
         const Mass q = mass_of(a.G + 1 + i);
-        q_d = q.power(Logits<DT>::widen(row_of<DT>(a, n, a.G + 1 + i)[d]), heat.c) * q.over();
+        q_d = q.power(q_at, heat.c) * q.over();
       }
-      rejected = !((double)a.uniforms[n * (a.G + 1) + i] * q_d < p.power(Logits<DT>::widen(row_of<DT>(a, n, i)[d]), heat.c) * p.over());
+      rejected = !((double)u * q_d < p.power(p_at, heat.c) * p.over());
     }
     const uint64_t mask = __ballot(rejected);
     if (mask != 0) {
@@ -626,8 +718,8 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) 
   }
   double* rest = a.rest + n * a.pieces;
   if (w.less) {
-    const int piece = group * W + wave, first = piece * a.piece_cols;
-    if (piece < a.pieces) {
+    for (int piece = group * W + wave; piece < a.pieces; piece += a.groups * W) {
+      const int first = piece * a.piece_cols;
       const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
       if (lane == 0) __hip_atomic_store(rest + piece, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
@@ -637,7 +729,7 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_join_kernel(DrawArgs a) 
     if (!last) return;
   }
   const int drawn = block_draw<DT, W>(
-      a, w, p, q, parts + (int64_t)pos * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
+      a, w, p, q, parts + (int64_t)kept(pos) * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
       (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }

@@ -92,12 +92,20 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
     for (a.row0 = 0; a.row0 < B && err == hipSuccess; a.row0 += most) err = launch(B - a.row0 < most ? B - a.row0 : most);
   };
   if (l.spread) {
+    a.groups = l.groups;
+    const int64_t rows = rtopk::kept_rows(G, draft, l), groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
     a.part = static_cast<double2*>(workspace);
-    a.rest = reinterpret_cast<double*>(a.part + B * rtopk::draw_rows(G, draft) * l.pieces);
+    a.rest = reinterpret_cast<double*>(a.part + B * rows * l.pieces);
     a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
-    const int64_t groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
-    sliced(rtopk::draw_rows(G, draft) * groups, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
-    sliced(groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
+    if (l.tested) {
+      a.accepts = reinterpret_cast<uint8_t*>(a.arrived + B);
+      for (int pos = 0; pos < G; pos += l.positions) {
+        const int positions = G - pos < l.positions ? G - pos : l.positions;
+        sliced(positions, [&](int64_t n) { return rtopk::launch_draw_test(dtype, l.test_waves, a, pos, positions, n, s); });
+      }
+    }
+    sliced(rows * groups, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
+    sliced(l.groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
   } else {
     sliced(1, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
   }

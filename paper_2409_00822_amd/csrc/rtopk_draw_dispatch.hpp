@@ -24,13 +24,16 @@ struct DrawArgs {
   int32_t* accepted;  // [B], optional
   int pieces, piece_cols;  // of a row
   // sequences spread over workgroups
-  double2* part;     // [B][rows][pieces] masses; rows: G + 1 of the target, G of the draft
+  int groups;        // workgroups that draw_join_kernel has for a sequence
+  double2* part;     // [B][rows][pieces] masses
   double* rest;      // [B][pieces] sums of max(p - q, 0)
   int32_t* arrived;  // [B]
+  uint8_t* accepts;  // [B][G] what the tests have accepted, null: no tests
 };
 
 // Each enqueues its kernel for sequences [a.row0, a.row0 + n).
 hipError_t launch_draw(int dtype, int waves, const DrawArgs& a, int64_t n, hipStream_t stream);  // a workgroup to a sequence
+hipError_t launch_draw_test(int dtype, int waves, const DrawArgs& a, int pos0, int positions, int64_t n, hipStream_t stream);
 hipError_t launch_draw_mass(int dtype, const DrawArgs& a, int64_t n, hipStream_t stream);
 hipError_t launch_draw_join(int dtype, const DrawArgs& a, int64_t n, hipStream_t stream);
 

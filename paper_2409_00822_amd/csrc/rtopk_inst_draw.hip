@@ -14,19 +14,34 @@ hipError_t draw_of_type(int waves, const DrawArgs& a, int64_t n, hipStream_t s) 
 }
 
 template <int DT>
+hipError_t test_of_type(int waves, const DrawArgs& a, int pos0, int positions, int64_t n, hipStream_t s) {
+  const dim3 grid((uint32_t)(n * positions)), block(64 * waves);
+  return waves == 4   ? launch_kernel(draw_test_kernel<DT, 4>, grid, block, 0, s, a, pos0, positions)
+         : waves == 8 ? launch_kernel(draw_test_kernel<DT, 8>, grid, block, 0, s, a, pos0, positions)
+                      : launch_kernel(draw_test_kernel<DT, 16>, grid, block, 0, s, a, pos0, positions);
+}
+
+template <int DT>
 hipError_t mass_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * draw_rows(a.G, a.draft != nullptr) * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
+  const int64_t rows = a.accepts ? (a.draft ? 2 : 1) : draw_rows(a.G, a.draft != nullptr);
+  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * rows * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 template <int DT>
 hipError_t join_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  return launch_kernel(draw_join_kernel<DT>, dim3((uint32_t)(n * (a.draft ? ceil_div(a.pieces, kDrawWaves) : 1))), dim3(64 * kDrawWaves), 0, s, a);
+  return launch_kernel(draw_join_kernel<DT, kDrawWaves>, dim3((uint32_t)(n * a.groups)), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_draw(int dtype, int waves, const DrawArgs& a, int64_t n, hipStream_t s) {
   return dtype == kF32 ? draw_of_type<kF32>(waves, a, n, s) : dtype == kF16 ? draw_of_type<kF16>(waves, a, n, s) : draw_of_type<kBF16>(waves, a, n, s);
+}
+
+hipError_t launch_draw_test(int dtype, int waves, const DrawArgs& a, int pos0, int positions, int64_t n, hipStream_t s) {
+  return dtype == kF32   ? test_of_type<kF32>(waves, a, pos0, positions, n, s)
+         : dtype == kF16 ? test_of_type<kF16>(waves, a, pos0, positions, n, s)
+                         : test_of_type<kBF16>(waves, a, pos0, positions, n, s);
 }
 
 hipError_t launch_draw_mass(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
