@@ -138,8 +138,9 @@ __device__ __forceinline__ Mass piece_mass(const typename Logits<DT>::elem* piec
   }
   for (; i - lane < g.chunks(); i += 64) {
     u4_vec w[1] = {u4_vec{L::kLow, L::kLow, L::kLow, L::kLow}};
-    if (i < g.full) w[0] = L::load(g.body + (uint32_t)i * L::V);
-    else if (i == g.full) w[0] = g.partial();
+    const int kind = chunk_kind(i, g.full, g.rest + g.lead);
+    if (kind == kWholeChunk) w[0] = L::load(g.body + (uint32_t)i * L::V);
+    else if (kind == kPartialChunk) w[0] = g.partial();
     masked |= i - lane + 64 > g.full;
     s += chunk_powers<DT, 1>(w, c, masked);
   }
@@ -314,16 +315,35 @@ template <int DT, int W>
 __device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int first, int cols, double before, double goal, FindRoom<W>& room) {
   constexpr int V = Logits<DT>::V, T = 64 * W;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  while (cols > T * V) {
-    const int part = ((cols + W - 1) / W + V - 1) / V * V, from = min(wave * part, cols);
-    const double s = piece_weight<DT>(w, p, q, first + from, min(part, cols - from), lane);
-    __syncthreads();
-    if (lane == 0) room.s[wave] = s;
-    __syncthreads();
-    const int j = passing(W, goal, before, [&](int i) { return room.s[i]; });
-    if (j < 0) return -1;
-    first += j * part;
-    cols = min(part, cols - j * part);
+  if constexpr (W == 1) {  // one wavefront: a part after the other
+    if (cols > T * V) {
+      int at = -1;
+      double all = before;
+      for (int from = 0; from < cols; from += T * V) {
+        const double s = piece_weight<DT>(w, p, q, first + from, min(T * V, cols - from), lane);
+        if (s > 0.0) {
+          at = from;
+          before = all;
+        }
+        all += s;
+        if (s > 0.0 && all > goal) break;
+      }
+      if (at < 0) return -1;
+      first += at;
+      cols = min(T * V, cols - at);
+    }
+  } else {
+    while (cols > T * V) {  // (a part is smaller: W > 1)
+      const int part = ((cols + W - 1) / W + V - 1) / V * V, from = min(wave * part, cols);
+      const double s = piece_weight<DT>(w, p, q, first + from, min(part, cols - from), lane);
+      __syncthreads();
+      if (lane == 0) room.s[wave] = s;
+      __syncthreads();
+      const int j = passing(W, goal, before, [&](int i) { return room.s[i]; });
+      if (j < 0) return -1;
+      first += j * part;
+      cols = min(part, cols - j * part);
+    }
   }
   double v[V], s = 0.0;
   int col = 0;
@@ -437,7 +457,7 @@ __device__ __forceinline__ void write_sequence(const DrawArgs& a, int64_t n, int
 // A sequence's temperature and its factor.
 struct Heat {
   double T, c;
-  __device__ __forceinline__ Heat(const DrawArgs& a, int64_t n) : T(a.temperatures ? (double)a.temperatures[n] : a.temperature), c(kLog2e64 / T) {}
+  __device__ __forceinline__ Heat(const DrawArgs& a, int64_t n) : T(a.temperatures ? (double)a.temperatures[n] : a.temperature), c(a.temperatures ? kLog2e64 / T : a.c) {}
   __device__ __forceinline__ bool certain() const { return T == 0.0; }
   __device__ __forceinline__ bool none() const { return !(T >= 0.0 && T < __builtin_inf()); }
 };
@@ -527,8 +547,9 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
 
 // ---- drafts tested beforehand ----------------------------------------------------------------------
 
-// fp32 sums of a row and the power at a draft are off by up to 64 units of 2^-24 each.  Where u q and p are nearer to each other than this part of them, they are
-// computed again in 64 bits.
+// fp32 sums of a row are off by less than 256 units of 2^-24: of up to 2^20 columns 256 threads add 128 batches each, one behind the other, of 16 terms to an
+// accumulator, and terms that weigh are off by some units each.  Where u q and p are nearer to each other than two rows' errors, they are computed again
+// in 64 bits.
 constexpr double kTestMargin = 0x1p-15;
 
 // The first of `most` positions whose draft the tests have rejected; each wavefront for itself.
@@ -564,13 +585,14 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
   } else {
     const double u = (double)a.uniforms[n * (a.G + 1) + pos];
     const float c = (float)heat.c;
-    const auto near = [&](const elem* x) {
+    const auto near = [&](const elem* x, int which) {
       const Segment<DT> g(x, a.M);
       const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, 4, false, false>(g, c), c, sums);
       __syncthreads();
+      if (threadIdx.x == 0) a.near[2 * (n * a.G + pos) + which] = make_float2(t.m, t.s);
       return power2(((double)Logits<DT>::widen(x[d]) - (double)t.m) * heat.c) / (double)t.s;
     };
-    double p_d = near(p), uq = a.draft ? u * near(q) : u;
+    double p_d = near(p, 0), uq = a.draft ? u * near(q, 1) : u;
     accepted = uq < p_d * (1.0 - kTestMargin);
     if (!accepted && !(uq > p_d * (1.0 + kTestMargin))) {
       const auto exact = [&](const elem* x) {
@@ -591,27 +613,24 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
 
 // ---- sequences spread over workgroups --------------------------------------------------------------
 
-// Rows of a sequence whose masses are kept: of all its positions, the target's first, or (tested) of the one that is drawn at.
-__device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.accepts ? (a.draft ? 2 : 1) : (a.draft ? 2 * a.G + 1 : a.G + 1); }
+// Rows of a sequence whose masses are kept: of all its positions, the target's first.
+__device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.draft ? 2 * a.G + 1 : a.G + 1; }
 
-// The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  Untested, all rows that may be looked at, those
-// behind a rejected draft among them: few sequences leave the GPU room for that.
+// The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  All rows that may be looked at, those behind a
+// rejected draft among them: few sequences leave the GPU room for that.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) {
   const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves, of = blockIdx.x / groups, rows = (uint32_t)rows_of(a);
-  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, kept = (int)(of % rows);
+  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, row = (int)(of % rows);
   const int64_t n = a.row0 + of / rows;
-  if (a.arrived && blockIdx.x % groups == 0 && kept == 0 && threadIdx.x == 0) a.arrived[n] = 0;
+  if (blockIdx.x % groups == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
   if (piece >= a.pieces) return;
   const Heat heat(a, n);
-  int row = kept;
-  if (heat.none()) return;
+  if (heat.none() || (heat.certain() && row > a.G)) return;
   if (a.G > 0) {
     const int g = drafts_of(a, n);
-    if (a.accepts) row = tested_up_to(a, n, g) + (kept == 0 ? 0 : a.G + 1);
     if (row <= a.G ? row > g : row - a.G - 1 >= g) return;
   }
-  if (heat.certain() && row > a.G) return;
   const auto* x = row_of<DT>(a, n, row);
   const int first = piece * a.piece_cols, cols = min(a.piece_cols, a.M - first);
   double2 out;
@@ -621,7 +640,7 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) 
     const Mass t = piece_mass<DT>(x + first, cols, lane, heat.c);
     out = make_double2(t.ref, t.s);
   }
-  if (lane == 0) a.part[(n * rows + kept) * a.pieces + piece] = out;
+  if (lane == 0) a.part[(n * rows + row) * a.pieces + piece] = out;
 }
 
 // Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
@@ -643,46 +662,44 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
     if (group == 0) write_sequence(a, n, 0, -1, T);
     return;
   }
-  const int g = a.G > 0 ? drafts_of(a, n) : 0, from = a.accepts ? tested_up_to(a, n, g) : 0, to = a.accepts ? from : g;  // positions whose masses there are
-  const auto kept = [&](int row) { return a.accepts ? (row <= a.G ? 0 : 1) : row; };
+  const int g = a.G > 0 ? drafts_of(a, n) : 0;
   const double2* parts = a.part + n * rows * a.pieces;
   if (heat.certain()) {
     if (group != 0) return;
-    for (int row = from + wave; row <= to; row += W) {
-      const int col = join_best(parts + (int64_t)kept(row) * a.pieces, a.pieces).col();
+    for (int row = wave; row <= g; row += W) {
+      const int col = join_best(parts + (int64_t)row * a.pieces, a.pieces).col();
       if (lane == 0) best[row] = col;
     }
     __syncthreads();
-    int pos = from;
-    while (pos < to && best[pos] >= 0 && best[pos] == draft_at(a, n, pos)) ++pos;
+    int pos = 0;
+    while (pos < g && best[pos] >= 0 && best[pos] == draft_at(a, n, pos)) ++pos;
     write_sequence(a, n, pos, best[pos], T);
     return;
   }
   // what the tests need, before the masses are there
   float p_at = 0.0f, q_at = 0.0f, u = 0.0f;
   const auto look = [&](int i) {
-    if (i < to) {
+    if (i < g) {
       const int d = draft_at(a, n, i);
       u = a.uniforms[n * (a.G + 1) + i];
       p_at = Logits<DT>::widen(row_of<DT>(a, n, i)[d]);
       if (a.draft) q_at = Logits<DT>::widen(row_of<DT>(a, n, a.G + 1 + i)[d]);
     }
   };
-  look(from + lane);
-  const int targets = to - from + 1, drafts = a.draft ? min(to + 1, g) - from : 0;
-  for (int i = wave; i < targets + drafts; i += W) {
-    const int row = i < targets ? from + i : a.G + 1 + from + i - targets;
-    const Mass t = join_mass(parts + (int64_t)kept(row) * a.pieces, a.pieces, heat.c);
+  look(lane);
+  for (int i = wave; i < (a.draft ? 2 * g + 1 : g + 1); i += W) {
+    const int row = i <= g ? i : a.G + i - g;
+    const Mass t = join_mass(parts + (int64_t)row * a.pieces, a.pieces, heat.c);
     if (lane == 0) mass[row] = make_double2(t.ref, t.s);
   }
   __syncthreads();
   const auto mass_of = [&](int row) { return Mass{mass[row].x, mass[row].y}; };
-  int pos = to;  // of the first rejected draft, or behind them all
-  for (int j = from; j < to; j += 64) {  // (untested)
+  int pos = g;  // of the first rejected draft, or behind them all
+  for (int j = 0; j < g; j += 64) {
     bool rejected = false;
     const int i = j + lane;
-    if (j > from) look(i);
-    if (i < to) {
+    if (j > 0) look(i);
+    if (i < g) {
       const Mass p = mass_of(i);
       double q_d = 1.0;
       if (a.draft) {
@@ -729,8 +746,161 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
     if (!last) return;
   }
   const int drawn = block_draw<DT, W>(
-      a, w, p, q, parts + (int64_t)kept(pos) * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
+      a, w, p, q, parts + (int64_t)pos * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
       (double)a.uniforms[n * (a.G + 1) + a.G], room);
+  write_sequence(a, n, pos, drawn, T);
+}
+
+// ---- the draws of tested sequences -----------------------------------------------------------------
+
+// With e_p and e_q the powers of two rows about 0, their sums S and l = S_p / S_q, a piece has  sum max(e_p - l e_q, 0) / S_p  of p - q.  That is taken in the pass
+// that finds the sums: about the tests' fp32 ratio k of them, A = sum max(e_p - k e_q, 0) and B = sum of e_q where that is not 0, so that
+// A - (l - k) B is the piece's sum but for columns between both ratios.  l and k differ by some 10^-6, and so do e_p and l e_q in such columns, which are as
+// many in 10^6: 10^-12 of the whole.
+struct Rest {
+  double p, q, a, b;
+};
+
+template <int DT>
+__device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int cols, int lane, double c, double ratio) {
+  using L = Logits<DT>;
+  Rest r = {0.0, 0.0, 0.0, 0.0};
+  const int full = cols / L::V, rest = cols % L::V;
+  bool masked = false;
+  const auto take = [&](float x, float y, Rest& t) {
+    const double ep = power2_finite((double)x * c), eq = power2_finite((double)y * c), d = __builtin_fma(-ratio, eq, ep);
+    t.p += ep;
+    t.q += eq;
+    t.a += fmax(d, 0.0);
+    t.b += d > 0.0 ? eq : 0.0;
+  };
+  const auto lowest = [](float x) { return x == kNegInf ? -3.402823466e38f : x; };
+  for (int i = lane; i - lane < full; i += 64) {
+    Rest t = {0.0, 0.0, 0.0, 0.0};
+    u4_vec x[1], y[1];
+    if (i < full) {
+      x[0] = L::load(p + (int64_t)i * L::V);
+      y[0] = L::load(q + (int64_t)i * L::V);
+      if (!masked) {
+#pragma unroll
+        for (int k = 0; k < L::V; ++k) take(L::at(x[0], k), L::at(y[0], k), t);
+      }
+    }
+    if (masked || __any(!(t.p + t.q == t.p + t.q))) {  // (-inf, or what is no number)
+      masked = true;
+      t = {0.0, 0.0, 0.0, 0.0};
+      if (i < full) {
+        apart(x);
+        apart(y);
+#pragma unroll
+        for (int k = 0; k < L::V; ++k) take(lowest(L::at(x[0], k)), lowest(L::at(y[0], k)), t);
+      }
+    }
+    r.p += t.p;
+    r.q += t.q;
+    r.a += t.a;
+    r.b += t.b;
+  }
+  if (lane < rest) take(lowest(L::widen(p[full * L::V + lane])), lowest(L::widen(q[full * L::V + lane])), r);
+  return {wave_sum(r.p), wave_sum(r.q), wave_sum(r.a), wave_sum(r.b)};
+}
+
+// S_p / S_q from the tests' fp32 sums.
+__device__ __forceinline__ double near_ratio(const DrawArgs& a, int64_t n, int pos, double c) {
+  const float2 p = a.near[2 * (n * a.G + pos)], q = a.near[2 * (n * a.G + pos) + 1];
+  return (double)p.y / (double)q.y * power2(((double)p.x - (double)q.x) * c);
+}
+
+// The pieces of the row that a sequence draws from, one to a wavefront: its mass, and that of the draft's row and what is left of p - q where a draft was rejected.
+template <int DT>
+__global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) {
+  const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves;
+  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t n = a.row0 + blockIdx.x / groups;
+  const Heat heat(a, n);
+  if (piece >= a.pieces || heat.none()) return;
+  const int g = drafts_of(a, n), pos = tested_up_to(a, n, g), first = piece * a.piece_cols, cols = min(a.piece_cols, a.M - first);
+  const auto* p = row_of<DT>(a, n, pos);
+  double2* part = a.part + 3 * n * a.pieces + piece;
+  if (heat.certain()) {
+    const Best b = piece_best<DT>(p, first, cols, lane);
+    if (lane == 0) *part = b.stored();
+  } else if (pos == g || !a.draft) {
+    const Mass t = piece_mass<DT>(p + first, cols, lane, heat.c);
+    if (lane == 0) *part = make_double2(t.ref, t.s);
+  } else {
+    const Rest r = piece_rest<DT>(p + first, row_of<DT>(a, n, a.G + 1 + pos) + first, cols, lane, heat.c, near_ratio(a, n, pos, heat.c));
+    if (lane == 0) {
+      *part = make_double2(0.0, r.p);
+      part[a.pieces] = make_double2(0.0, r.q);
+      part[2 * a.pieces] = make_double2(r.a, r.b);
+    }
+  }
+}
+
+// The draw of a sequence from those.
+template <int DT>
+__global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) {
+  using elem = typename Logits<DT>::elem;
+  constexpr int W = kDrawWaves, T = 64 * W;
+  __shared__ FindRoom<W> room;
+  const int64_t n = a.row0 + blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Heat heat(a, n);
+  if (heat.none()) {
+    write_sequence(a, n, 0, -1, T);
+    return;
+  }
+  const int g = drafts_of(a, n), pos = tested_up_to(a, n, g);
+  double2 *part = a.part + 3 * n * a.pieces, *draft_part = part + a.pieces, *rest = part + 2 * a.pieces;
+  if (heat.certain()) {
+    write_sequence(a, n, pos, join_best(part, a.pieces).col(), T);
+    return;
+  }
+  Weights w;
+  w.c = heat.c;
+  w.p = join_mass(part, a.pieces, w.c);
+  w.over_p = w.p.over();
+  w.without = pos < g && !a.draft ? draft_at(a, n, pos) : -1;
+  w.less = pos < g && a.draft;
+  const elem *p = row_of<DT>(a, n, pos), *q = p;
+  double more = 0.0;  // l - k
+  if (w.less) {
+    q = row_of<DT>(a, n, a.G + 1 + pos);
+    w.q = join_mass(draft_part, a.pieces, w.c);
+    const double k = near_ratio(a, n, pos, w.c), l = w.p.s / w.q.s;
+    const auto in_range = [](double s) { return s >= kLeastSum && s <= kMostSum; };
+    if (in_range(w.p.s) && in_range(w.q.s) && fabs(l - k) <= kTestMargin * l) {
+      more = l - k;
+    } else {  // sums about 0 leave their range, or there are none: about the maxima, here
+      __syncthreads();
+      for (int j = wave; j < a.pieces; j += W) {
+        const int first = j * a.piece_cols, cols = min(a.piece_cols, a.M - first);
+        const Mass s = piece_mass<DT>(p + first, cols, lane, w.c), t = piece_mass<DT>(q + first, cols, lane, w.c);
+        if (lane == 0) {
+          part[j] = make_double2(s.ref, s.s);
+          draft_part[j] = make_double2(t.ref, t.s);
+        }
+      }
+      __syncthreads();
+      w.p = join_mass(part, a.pieces, w.c);
+      w.q = join_mass(draft_part, a.pieces, w.c);
+      w.over_p = w.p.over();
+      w.over_q = w.q.over();
+      if (w.is_number()) {
+        for (int j = wave; j < a.pieces; j += W) {
+          const int first = j * a.piece_cols;
+          const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
+          if (lane == 0) rest[j] = make_double2(w.p.s * s, 0.0);
+        }
+      }
+      __syncthreads();
+    }
+    w.over_q = w.q.over();
+  }
+  int drawn = -1;
+  if (w.is_number())
+    drawn = block_draw<DT, W>(a, w, p, q, part, [&](int j) { return fmax(__builtin_fma(-more, rest[j].y, rest[j].x), 0.0) * w.over_p; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }
 

@@ -76,6 +76,7 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
   a.uniforms = uniforms;
   a.temperatures = temperatures;
   a.temperature = temperature;
+  a.c = 1.44269504088896340736 / temperature;
   a.B = B;
   a.tokens = out_tokens;
   a.accepted = out_accepted;
@@ -93,19 +94,25 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
   };
   if (l.spread) {
     a.groups = l.groups;
-    const int64_t rows = rtopk::kept_rows(G, draft, l), groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
+    const int64_t rows = rtopk::kept_rows(G, draft, l);
     a.part = static_cast<double2*>(workspace);
-    a.rest = reinterpret_cast<double*>(a.part + B * rows * l.pieces);
-    a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
     if (l.tested) {
-      a.accepts = reinterpret_cast<uint8_t*>(a.arrived + B);
-      for (int pos = 0; pos < G; pos += l.positions) {
-        const int positions = G - pos < l.positions ? G - pos : l.positions;
+      const int64_t groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
+      a.near = reinterpret_cast<float2*>(a.part + B * rows * l.pieces);
+      a.accepts = reinterpret_cast<uint8_t*>(a.near + 2 * B * G);
+      for (int pos = 0, launch = 0, positions; pos < G; pos += positions, ++launch) {
+        positions = l.positions + launch / 2;
+        if (positions > G - pos) positions = G - pos;
         sliced(positions, [&](int64_t n) { return rtopk::launch_draw_test(dtype, l.test_waves, a, pos, positions, n, s); });
       }
+      sliced(groups, [&](int64_t n) { return rtopk::launch_draw_rest(dtype, a, n, s); });
+      sliced(1, [&](int64_t n) { return rtopk::launch_draw_pick(dtype, a, n, s); });
+    } else {
+      a.rest = reinterpret_cast<double*>(a.part + B * rows * l.pieces);
+      a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
+      sliced(rows * rtopk::ceil_div(l.pieces, rtopk::kDrawWaves), [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
+      sliced(l.groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
     }
-    sliced(rows * groups, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
-    sliced(l.groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
   } else {
     sliced(1, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
   }

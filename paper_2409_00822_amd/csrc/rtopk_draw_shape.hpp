@@ -10,13 +10,17 @@ namespace rtopk {
 
 constexpr int kMaxDrafts = 128;  // drafted tokens of a sequence
 
+// What chunk i of a piece is that has `full` whole ones and `left` columns beside them.
+enum ChunkKind { kNoChunk = 0, kWholeChunk = 1, kPartialChunk = 2 };
+constexpr int chunk_kind(int i, int full, int left) { return i < full ? kWholeChunk : (i == full && left != 0 ? kPartialChunk : kNoChunk); }
+
 constexpr int kDrawWaves = 4;    // of a workgroup that shares a sequence with others
 constexpr int kMostPieces = 64;  // of a row that one workgroup takes
-constexpr int64_t kTestedCells = (int64_t)1 << 26;  // logits of a call from which on drafts are tested in fp32 first
+constexpr int kMostTested = 1 << 20;  // columns of rows that are tested in fp32: the sums' errors are bounded for that many
 
 // A row in `pieces` pieces of `cols` columns (the last one what is left), a whole number of 128-bit loads of a wavefront.  spread: a wavefront of any workgroup
-// to a piece; else a workgroup of `waves` wavefronts to a sequence.  tested: drafts are tested in fp32 beforehand, `positions` of each sequence in a
-// launch, by workgroups of `test_waves` wavefronts.
+// to a piece; else a workgroup of `waves` wavefronts to a sequence.  tested: drafts are tested in fp32 beforehand, `positions` of each sequence in the first
+// two launches, one more in the next two, and so on, by workgroups of `test_waves` wavefronts.
 struct DrawLayout {
   bool spread;
   int waves, pieces, cols;
@@ -26,8 +30,8 @@ struct DrawLayout {
 };
 
 inline int draw_rows(int G, bool draft) { return draft ? 2 * G + 1 : G + 1; }
-// Rows of a sequence whose pieces' masses are kept.
-inline int kept_rows(int G, bool draft, const DrawLayout& l) { return l.tested ? (draft ? 2 : 1) : draw_rows(G, draft); }
+// Rows of pieces' results that are kept of a sequence.
+inline int kept_rows(int G, bool draft, const DrawLayout& l) { return l.tested ? 3 : draw_rows(G, draft); }
 
 // Pieces of `loads` loads, more where there would be more than `most` pieces.
 inline DrawLayout draw_pieces(int M, int dtype, int64_t loads, int most) {
@@ -36,39 +40,59 @@ inline DrawLayout draw_pieces(int M, int dtype, int64_t loads, int most) {
   return {false, 4, (int)ceil_div(M, loads * step), (int)(loads * step), 1, false, 0, 0};
 }
 
+// One wavefront to a short sequence where there are many, which pays no barriers (tokens of 16384 rows of 1000 bfloat16 logits 41 us, with four 94; 1024 rows
+// 7.4 and 8.7, 64 rows 6.7 and 6.5; 4096 x 8000 43 and 49, 1024 x 8000 21 and 16); else four for short rows or many, eight for few of up to 8192
+// columns, sixteen for few wide ones.
 inline DrawLayout draw_layout_whole(int64_t B, int M, int dtype) {
   DrawLayout l = draw_pieces(M, dtype, 1, kMostPieces);
-  l.waves = M <= 2048 || B > 512 ? 4 : (B > 256 ? 8 : 16);
+  if (M <= 8192) l.waves = 2 * B >= M ? 1 : (M <= 2048 || B > 256 ? 4 : 8);
+  else l.waves = B > 512 ? 4 : (B > 256 ? 8 : 16);
   return l;
+}
+
+// One workgroup to a sequence, us against spread ones: tokens of rows of up to 8192 columns (1 x 8000 bfloat16 7.8 and 8.8, 1024 x 4000 11.7 and 13.2; 64 x 32000 15.1 and
+// 10.6, 4096 x 32000 130 and 107); drafts where rows are short and few (256 sequences of one draft, 1000 columns 10.2 and 13.5, 4000 12.1 and 16.5; of four
+// drafts 20.1 and 16.5) or sequences many (4096 of four drafts, 1000 columns 56 and 98).
+inline bool by_workgroups(int64_t B, int G, int M) {
+  if (B > 16384) return true;
+  if (G == 0) return M <= 8192;
+  return G <= 2 ? M <= 4096 : (M <= 2048 && B >= 1024);
+}
+
+// Drafts tested beforehand, us against all rows' sums in 64 bits, four drafts: bfloat16, 32000 columns 16 sequences 20.5 and 17.4, 32 21.3 and 21.8, 64 24.5 and 28.0, 256 53.7
+// and 70.9; 131072 columns 16 sequences 37.8 and 29.3, 32 39.1 and 44.3, 64 47.7 and 71.8, 256 131 and 260; fp32, 32000 columns 32 sequences 24.7 and 21.0, 128 40.9 and
+// 46.1, 131072 columns 16 sequences 47.0 and 32.5, 64 69.5 and 91.0.  A workgroup to a row is slow for few wide rows.  Narrower rows only where they are
+// many (8000 columns, eight drafts, 256 sequences 48.4 and 40.3; 4000 columns, four drafts, 4096 sequences 135 and 178).
+inline bool test_first(int64_t B, int G, int M, int dtype, bool draft) {
+  const int64_t cells = B * draw_rows(G, draft) * M, least = (int64_t)256 * M;
+  return G > 0 && M <= kMostTested && (M >= 16384 || B >= 1024) && cells >= (least > (1 << 23) ? least : 1 << 23) + (dtype == 0 ? 1 << 23 : 0);
 }
 
 inline DrawLayout draw_layout(int64_t B, int G, int M, int dtype, bool draft) {
-  DrawLayout l = draw_layout_whole(B, M, dtype);
-  if (B > 16384 || l.pieces <= 4) return l;
+  if (by_workgroups(B, G, M)) return draw_layout_whole(B, M, dtype);
   const int64_t rows = draw_rows(G, draft), row = 64 * logits_width(dtype);
-  const bool tested = rows >= 5 && B * rows * M >= kTestedCells;
-  int64_t loads = 1;
-  while (loads < 4 && B * (tested ? (draft ? 2 : 1) : rows) * ceil_div(M, 2 * loads * row) >= 4096) loads *= 2;
-  l = draw_pieces(M, dtype, loads, 1024);
+  const bool tested = test_first(B, G, M, dtype, draft);
+  int64_t loads = 1;  // of a piece: four where that makes enough wavefronts
+  while (loads < 4 && B * (tested ? 1 : rows) * ceil_div(M, 2 * loads * row) >= 4096) loads *= 2;
+  DrawLayout l = draw_pieces(M, dtype, loads, 1024);
   l.spread = true;
-  if (draft) {
-    l.groups = (int)ceil_div(l.pieces, kDrawWaves);
-    if (B * l.groups > 1024) l.groups = B < 1024 ? (int)(1024 / B) : 1;
-  }
   if (tested) {
     l.tested = true;
     l.positions = (int)(B < 512 ? ceil_div(512, B) : 1);
-    if (l.positions > G) l.positions = G;
     const int64_t workgroups = B * l.positions;
     l.test_waves = workgroups <= 256 ? 16 : (workgroups <= 512 ? 8 : 4);
+  } else if (draft) {
+    l.groups = (int)ceil_div(l.pieces, kDrawWaves);
+    if (B * l.groups > 1024) l.groups = B < 1024 ? (int)(1024 / B) : 1;
   }
   return l;
 }
 
-// Device memory: masses of the pieces, their sums of max(p - q, 0), a counter for each sequence, what the tests have accepted.
+// Device memory: the pieces' results; untested their sums of max(p - q, 0) and a counter for each sequence; tested the drafts' fp32 sums and what is accepted.
 inline int64_t draw_workspace(int64_t B, int G, bool draft, const DrawLayout& l) {
   if (!l.spread) return 0;
-  return B * l.pieces * (16 * (int64_t)kept_rows(G, draft, l) + 8) + 4 * B + (l.tested ? B * G : 0);
+  const int64_t parts = B * l.pieces * 16 * (int64_t)kept_rows(G, draft, l);
+  return l.tested ? parts + 17 * B * G : parts + 8 * B * l.pieces + 4 * B;
 }
 
 }  // namespace rtopk

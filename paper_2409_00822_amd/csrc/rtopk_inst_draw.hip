@@ -8,7 +8,8 @@ namespace {
 template <int DT>
 hipError_t draw_of_type(int waves, const DrawArgs& a, int64_t n, hipStream_t s) {
   const dim3 grid((uint32_t)n), block(64 * waves);
-  return waves == 4   ? launch_kernel(draw_kernel<DT, 4>, grid, block, 0, s, a)
+  return waves == 1   ? launch_kernel(draw_kernel<DT, 1>, grid, block, 0, s, a)
+         : waves == 4 ? launch_kernel(draw_kernel<DT, 4>, grid, block, 0, s, a)
          : waves == 8 ? launch_kernel(draw_kernel<DT, 8>, grid, block, 0, s, a)
                       : launch_kernel(draw_kernel<DT, 16>, grid, block, 0, s, a);
 }
@@ -23,8 +24,18 @@ hipError_t test_of_type(int waves, const DrawArgs& a, int pos0, int positions, i
 
 template <int DT>
 hipError_t mass_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  const int64_t rows = a.accepts ? (a.draft ? 2 : 1) : draw_rows(a.G, a.draft != nullptr);
+  const int64_t rows = draw_rows(a.G, a.draft != nullptr);
   return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * rows * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
+}
+
+template <int DT>
+hipError_t rest_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
+  return launch_kernel(draw_rest_kernel<DT>, dim3((uint32_t)(n * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
+}
+
+template <int DT>
+hipError_t pick_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
+  return launch_kernel(draw_pick_kernel<DT>, dim3((uint32_t)n), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 template <int DT>
@@ -50,6 +61,14 @@ hipError_t launch_draw_mass(int dtype, const DrawArgs& a, int64_t n, hipStream_t
 
 hipError_t launch_draw_join(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
   return dtype == kF32 ? join_of_type<kF32>(a, n, s) : dtype == kF16 ? join_of_type<kF16>(a, n, s) : join_of_type<kBF16>(a, n, s);
+}
+
+hipError_t launch_draw_rest(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
+  return dtype == kF32 ? rest_of_type<kF32>(a, n, s) : dtype == kF16 ? rest_of_type<kF16>(a, n, s) : rest_of_type<kBF16>(a, n, s);
+}
+
+hipError_t launch_draw_pick(int dtype, const DrawArgs& a, int64_t n, hipStream_t s) {
+  return dtype == kF32 ? pick_of_type<kF32>(a, n, s) : dtype == kF16 ? pick_of_type<kF16>(a, n, s) : pick_of_type<kBF16>(a, n, s);
 }
 
 }  // namespace rtopk

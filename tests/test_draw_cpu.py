@@ -1,10 +1,12 @@
 """Drawn tokens and verified drafts without a GPU: arguments refused on the host, and the definitions themselves (oracle/draw.py): tokens that come out of
 verified drafts are distributed as the target's."""
 import os
+import subprocess
 
 import numpy as np
 import pytest
 
+from conftest import ROOT
 from oracle import draw as definition
 
 
@@ -120,3 +122,91 @@ def test_hand_traces():
     assert definition.verify(x, [0], [0.9, 0.9], q, 0.0)[:2] == ([0, 2], 1)
     assert definition.verify(x, [1], [0.0, 0.9], q, 0.0)[:2] == ([0, -1], 0)
     assert definition.verify(x, [-1], [0.0, 0.6], q, 1.0)[:2] == ([1, -1], 0)
+
+
+CHUNKS = r"""
+#include <stdio.h>
+#include "rtopk_draw_shape.hpp"
+using namespace rtopk;
+// The columns that the lanes of a wavefront read of a piece (piece_mass): each of the piece once, none beyond it.
+int main() {
+  long bad = 0;
+  for (int V = 4; V <= 8; V += 4)
+    for (int lead = 0; lead <= (V == 8); ++lead)
+      for (int cols = 1; cols <= 4096; ++cols) {
+        static int seen[4200];
+        for (int c = 0; c < 4200; ++c) seen[c] = 0;
+        const int full = (cols - lead) / V, rest = (cols - lead) % V, chunks = full + (rest + lead != 0), U = V == 4 ? 4 : 2;
+        for (int lane = 0; lane < 64; ++lane) {
+          int i = lane;
+          const auto whole = [&](int chunk) { for (int c = 0; c < V; ++c) ++seen[lead + chunk * V + c]; };
+          for (; i - lane + U * 64 <= full; i += U * 64)
+            for (int u = 0; u < U; ++u) whole(i + u * 64);
+          for (; i - lane < chunks; i += 64) {
+            const int kind = chunk_kind(i, full, rest + lead);
+            if (kind == kWholeChunk) whole(i);
+            if (kind == kPartialChunk) {
+              if (rest + lead == 0) ++bad;  // its loads for columns that it has not go to one that it has
+              for (int c = 0; c < rest; ++c) ++seen[lead + full * V + c];
+              if (lead) ++seen[0];
+            }
+          }
+        }
+        for (int c = 0; c < 4200; ++c) bad += seen[c] != (c < cols);
+      }
+  printf("%ld\n", bad);
+  return bad != 0;
+}
+"""
+
+
+def test_the_lanes_of_a_piece_read_its_columns_and_no_others(tmp_path):
+    src = tmp_path / "chunks.cpp"
+    src.write_text(CHUNKS)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-I" + os.path.join(ROOT, "paper_2409_00822_amd", "csrc"), str(src), "-o", str(tmp_path / "chunks")])
+    out = subprocess.run([str(tmp_path / "chunks")], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
+
+
+LAYOUTS = r"""
+#include <stdio.h>
+#include "rtopk_draw_shape.hpp"
+using namespace rtopk;
+int main() {
+  long bad = 0, all = 0, tested = 0, spread = 0;
+  const int64_t counts[] = {1, 2, 3, 16, 63, 64, 255, 256, 511, 512, 513, 1000, 1024, 4096, 16384, 16385, 100000, (int64_t)1 << 31};
+  const int drafts[] = {0, 1, 2, 3, 7, 64, 128};
+  for (int dtype = 0; dtype < 3; ++dtype)
+    for (int64_t M = 1; M <= kMaxLogitsM; M += M < 20000 ? 7 : M / 97)
+      for (int64_t B : counts)
+        for (int G : drafts)
+          for (int draft = 0; draft <= (G > 0); ++draft) {
+            const DrawLayout l = draw_layout(B, G, (int)M, dtype, draft);
+            ++all;
+            tested += l.tested;
+            spread += l.spread;
+            // every column in one piece, none empty, whole loads of a wavefront
+            if (l.pieces < 1 || (int64_t)l.pieces * l.cols < M || (int64_t)(l.pieces - 1) * l.cols >= M || l.cols % (64 * logits_width(dtype)) != 0) ++bad;
+            if (l.pieces > (l.spread ? 1024 : kMostPieces)) ++bad;
+            if (l.waves != 1 && l.waves != 4 && l.waves != 8 && l.waves != 16) ++bad;
+            if (l.tested && (!l.spread || G == 0 || M > kMostTested || l.positions < 1 || (l.test_waves != 4 && l.test_waves != 8 && l.test_waves != 16))) ++bad;
+            if (l.groups < 1 || (l.spread && l.groups > (l.pieces + kDrawWaves - 1) / kDrawWaves)) ++bad;
+            // a sequence's workgroups fit a launch
+            if (l.spread && (int64_t)draw_rows(G, draft) * ((l.pieces + kDrawWaves - 1) / kDrawWaves) > (1 << 21)) ++bad;
+            const int64_t bytes = draw_workspace(B, G, draft, l);
+            if (bytes < 0 || (l.spread ? bytes < 16 * B * l.pieces : bytes != 0)) ++bad;
+            const DrawLayout w = draw_layout_whole(B, (int)M, dtype);
+            if (w.spread || w.pieces > kMostPieces || (int64_t)w.pieces * w.cols < M) ++bad;
+          }
+  printf("%ld of %ld, %ld spread, %ld tested\n", bad, all, spread, tested);
+  return bad != 0 || tested == 0 || spread == 0;
+}
+"""
+
+
+def test_layouts(tmp_path):
+    src = tmp_path / "layouts.cpp"
+    src.write_text(LAYOUTS)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-I" + os.path.join(ROOT, "paper_2409_00822_amd", "csrc"), str(src), "-o", str(tmp_path / "layouts")])
+    out = subprocess.run([str(tmp_path / "layouts")], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
