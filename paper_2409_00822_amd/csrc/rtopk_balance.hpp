@@ -458,7 +458,7 @@ __global__ __launch_bounds__(T) void balance_join_kernel(BalanceArgs a) {
   if (blocks > 1) {
     double* dots = a.part_dot + (int64_t)g * blocks;
     __hip_atomic_store(dots + block, dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");  // (the store is done)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the store is done (a fence of the workgroup would not wait for it)
     if (__hip_atomic_fetch_add(a.arrived + g, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != blocks - 1) return;
     dot = 0.0;
     for (int i = 0; i < blocks; ++i) dot += __hip_atomic_load(dots + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

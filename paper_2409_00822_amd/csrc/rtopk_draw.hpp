@@ -46,6 +46,8 @@ __device__ __forceinline__ double power2_finite(double t) {
 }
 // The same with 0 for -inf; NaN stays.
 __device__ __forceinline__ double power2(double t) { return power2_finite(t < -1100.0 ? -1100.0 : t); }
+// 2^(x c), 0 for a masked x at any c (one that is finite may be the type's lowest value and weigh something at a very high temperature).
+__device__ __forceinline__ double masked_power(float x, double c) { return power2_finite(x == kNegInf ? -1100.0 : (double)x * c); }
 
 // A 64-bit value moved by a DPP permutation, 0 where it comes from no lane.
 template <int CTRL, int ROWS>
@@ -78,12 +80,15 @@ struct Mass {
   __device__ __forceinline__ double over() const { return s == 0.0 ? 0.0 : 1.0 / s; }
 };
 
+// Waits until the wavefront's stores are where those of other workgroups are: in memory, if they were made past the caches.
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // ---- pieces of rows -------------------------------------------------------------------------------
 
 // A row is cut into pieces of a whole number of 128-bit loads of a wavefront (draw_pieces); a wavefront sums a piece, and what a row's pieces sum to says
 // which of them a draw falls in.
 
-// Sum of the powers about 0 of U chunks.  Masked columns make it NaN; it is then taken again with -inf as the type's lowest value, and so are all that follow.
+// Sum of the powers about 0 of U chunks.  Masked columns make it NaN; it is then taken again with nothing for -inf, and so are all that follow.
 template <int DT, int U>
 __device__ __forceinline__ double chunk_powers(u4_vec (&w)[U], double c, bool& masked) {
   using L = Logits<DT>;
@@ -99,10 +104,7 @@ __device__ __forceinline__ double chunk_powers(u4_vec (&w)[U], double c, bool& m
 #pragma unroll 1
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < L::V; ++i) {
-        const float x = L::at(w[u], i);
-        a[i & 1] += power2_finite((double)(x == kNegInf ? -3.402823466e38f : x) * c);
-      }
+      for (int i = 0; i < L::V; ++i) a[i & 1] += masked_power(L::at(w[u], i), c);
   }
   return a[0] + a[1];
 }
@@ -249,7 +251,7 @@ __device__ __forceinline__ void each_weight(const Weights& w, const typename Log
   const auto *a = p + first, *b = (w.less ? q : p) + first;
   double v[L::V];
   if (w.less && w.p.ref == 0.0 && w.q.ref == 0.0) {  // (mostly; neither row has a NaN or +inf)
-    const auto power = [&](float x) { return power2_finite((double)fmaxf(x, -3.402823466e38f) * w.c); };
+    const auto power = [&](float x) { return power2_finite(fmax((double)x * w.c, -1100.0)); };
     for (; i < full; i += T) {
       const u4_vec x = L::load(a + (int64_t)i * L::V), y = L::load(b + (int64_t)i * L::V);
 #pragma unroll
@@ -547,10 +549,10 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
 
 // ---- drafts tested beforehand ----------------------------------------------------------------------
 
-// fp32 sums of a row are off by less than 256 units of 2^-24: of up to 2^20 columns 256 threads add 128 batches each, one behind the other, of 16 terms to an
-// accumulator, and terms that weigh are off by some units each.  Where u q and p are nearer to each other than two rows' errors, they are computed again
+// fp32 sums of a row are off by less than 512 units of 2^-24: of up to 2^20 columns 256 threads add up to 256 batches each, one behind the other, of 16 terms
+// to an accumulator, and terms that weigh are off by some tens of units each.  Where u q and p are nearer to each other than two rows' errors, they are computed again
 // in 64 bits.
-constexpr double kTestMargin = 0x1p-15;
+constexpr double kTestMargin = 0x1p-14;
 
 // The first of `most` positions whose draft the tests have rejected; each wavefront for itself.
 __device__ __forceinline__ int tested_up_to(const DrawArgs& a, int64_t n, int most) {
@@ -740,7 +742,9 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
       const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
       if (lane == 0) __hip_atomic_store(rest + piece, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();  // (the stores are done: they, and the loads of the last workgroup, go past the caches, which need not be written back then)
+    // the stores, and the loads of the last workgroup, go past the caches, which need not be written back then; a barrier alone does not wait for stores
+    stores_done();
+    __syncthreads();
     if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.arrived + n, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)groups - 1;
     __syncthreads();
     if (!last) return;
@@ -755,28 +759,36 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
 
 // With e_p and e_q the powers of two rows about 0, their sums S and l = S_p / S_q, a piece has  sum max(e_p - l e_q, 0) / S_p  of p - q.  That is taken in the pass
 // that finds the sums: about the tests' fp32 ratio k of them, A = sum max(e_p - k e_q, 0) and B = sum of e_q where that is not 0, so that
-// A - (l - k) B is the piece's sum but for columns between both ratios.  l and k differ by some 10^-6, and so do e_p and l e_q in such columns, which are as
-// many in 10^6: 10^-12 of the whole.
+// A - (l - k) B is the piece's sum if no column's ratio lies between l and k.  A piece that has a column nearer to k than l may be, k kNearRatio (rows
+// that are alike in most columns have many), is marked, and summed again when l is known.
 struct Rest {
   double p, q, a, b;
+  bool near;
 };
+constexpr int kNearBits = 18;  // l and k differ by 10^-7 to 10^-6 of them; a piece of 2048 columns whose ratios spread over two octaves is marked one time in 200
+constexpr double kNearRatio = 1.0 / (1 << kNearBits);
 
 template <int DT>
 __device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int cols, int lane, double c, double ratio) {
   using L = Logits<DT>;
-  Rest r = {0.0, 0.0, 0.0, 0.0};
+  Rest r = {0.0, 0.0, 0.0, 0.0, false};
   const int full = cols / L::V, rest = cols % L::V;
+  const double far = ratio * (1 << kNearBits);  // e_q is kept times kNearRatio: what e_p - k e_q is held against
   bool masked = false;
-  const auto take = [&](float x, float y, Rest& t) {
-    const double ep = power2_finite((double)x * c), eq = power2_finite((double)y * c), d = __builtin_fma(-ratio, eq, ep);
+  const auto add = [&](double ep, double eq, Rest& t) {
+    const double d = __builtin_fma(-far, eq, ep);
     t.p += ep;
     t.q += eq;
     t.a += fmax(d, 0.0);
     t.b += d > 0.0 ? eq : 0.0;
+    t.near |= fabs(d) < ratio * eq;
   };
-  const auto lowest = [](float x) { return x == kNegInf ? -3.402823466e38f : x; };
+  const auto take = [&](float x, float y, Rest& t) { add(power2_finite((double)x * c), power2_finite(__builtin_fma((double)y, c, -(double)kNearBits)), t); };
+  const auto take_masked = [&](float x, float y, Rest& t) {
+    add(masked_power(x, c), power2_finite(y == kNegInf ? -1100.0 : __builtin_fma((double)y, c, -(double)kNearBits)), t);
+  };
   for (int i = lane; i - lane < full; i += 64) {
-    Rest t = {0.0, 0.0, 0.0, 0.0};
+    Rest t = {0.0, 0.0, 0.0, 0.0, false};
     u4_vec x[1], y[1];
     if (i < full) {
       x[0] = L::load(p + (int64_t)i * L::V);
@@ -788,21 +800,22 @@ __device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, c
     }
     if (masked || __any(!(t.p + t.q == t.p + t.q))) {  // (-inf, or what is no number)
       masked = true;
-      t = {0.0, 0.0, 0.0, 0.0};
+      t = {0.0, 0.0, 0.0, 0.0, false};
       if (i < full) {
         apart(x);
         apart(y);
 #pragma unroll
-        for (int k = 0; k < L::V; ++k) take(lowest(L::at(x[0], k)), lowest(L::at(y[0], k)), t);
+        for (int k = 0; k < L::V; ++k) take_masked(L::at(x[0], k), L::at(y[0], k), t);
       }
     }
     r.p += t.p;
     r.q += t.q;
     r.a += t.a;
     r.b += t.b;
+    r.near |= t.near;
   }
-  if (lane < rest) take(lowest(L::widen(p[full * L::V + lane])), lowest(L::widen(q[full * L::V + lane])), r);
-  return {wave_sum(r.p), wave_sum(r.q), wave_sum(r.a), wave_sum(r.b)};
+  if (lane < rest) take_masked(L::widen(p[full * L::V + lane]), L::widen(q[full * L::V + lane]), r);
+  return {wave_sum(r.p), wave_sum(r.q) * (1 << kNearBits), wave_sum(r.a), wave_sum(r.b) * (1 << kNearBits), (bool)__any(r.near)};
 }
 
 // S_p / S_q from the tests' fp32 sums.
@@ -833,7 +846,7 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) 
     if (lane == 0) {
       *part = make_double2(0.0, r.p);
       part[a.pieces] = make_double2(0.0, r.q);
-      part[2 * a.pieces] = make_double2(r.a, r.b);
+      part[2 * a.pieces] = make_double2(r.a, r.near ? -r.b : r.b);  // (a sign marks it)
     }
   }
 }
@@ -870,8 +883,19 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) 
     w.q = join_mass(draft_part, a.pieces, w.c);
     const double k = near_ratio(a, n, pos, w.c), l = w.p.s / w.q.s;
     const auto in_range = [](double s) { return s >= kLeastSum && s <= kMostSum; };
-    if (in_range(w.p.s) && in_range(w.q.s) && fabs(l - k) <= kTestMargin * l) {
+    if (in_range(w.p.s) && in_range(w.q.s) && fabs(l - k) < kNearRatio * k) {
       more = l - k;
+      w.over_q = w.q.over();
+      for (int j0 = 0; j0 < a.pieces; j0 += 64) {  // a wavefront takes each W-th piece that is marked
+        const int mine = j0 + lane;
+        uint64_t marked = __ballot(mine < a.pieces && mine % W == wave && __double_as_longlong(rest[min(mine, a.pieces - 1)].y) < 0);
+        for (; marked != 0; marked &= marked - 1) {
+          const int j = j0 + __builtin_ctzll(marked), first = j * a.piece_cols;
+          const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
+          if (lane == 0) rest[j] = make_double2(w.p.s * s, 0.0);
+        }
+      }
+      __syncthreads();
     } else {  // sums about 0 leave their range, or there are none: about the maxima, here
       __syncthreads();
       for (int j = wave; j < a.pieces; j += W) {

@@ -159,6 +159,27 @@ def test_far_temperatures(dtype, T):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("B,M", [(3, 1003), (2, 40000), (300, 16400)])
+@pytest.mark.parametrize("T", [3e35, 1e38, 1e300])
+def test_masks_at_temperatures_that_make_all_alike(dtype, B, M, T):
+    """A masked column has no probability at any temperature, nor does it at one where the type's lowest value would have some."""
+    R = _gpu()
+    target = block((B, 3, M), dtype, 5)
+    draft = block((B, 2, M), dtype, 6)
+    target[:, :, ::2] = -float("inf")
+    draft[:, :, 1::2] = -float("inf")
+    draft[::2, :, : M // 3] = 1.0
+    drafts = drawn_from(draft.clamp(min=-1e4), 1.0, 4)
+    u = numbers((B, 3), 8)
+    some = slice(0, 12)
+    check_sample(R, target[some, 0], u[some, 0].contiguous(), T)
+    check_verify(R, target[some], drafts[some], u[some], draft[some], T)
+    tokens, accepted = R.rtopk_verify_drafts(target, drafts, u, draft, T)
+    drawn = tokens.gather(1, accepted.long()[:, None])
+    assert (tokens[tokens >= 0] % 2 == 1).all() and (drawn >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("B,G,M,pad,shift", [(1, 1, 2, 0, 0), (3, 2, 5, 1, 1), (7, 1, 64, 0, 0), (5, 4, 1000, 0, 0), (9, 8, 1003, 5, 1), (2, 3, 32000, 0, 0), (2, 5, 50001, 1, 1),
                                              (40, 3, 999, 0, 0), (1, 128, 70, 0, 0)])
 @pytest.mark.parametrize("T", [1.0, 0.6, "mixed"])

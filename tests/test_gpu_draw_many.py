@@ -133,6 +133,30 @@ def test_numbers_at_the_tests_border():
     assert torch.equal(got[1] > 0, accepted) and 0 < int(accepted.sum()) < B
 
 
+@pytest.mark.parametrize("dtype,M", [("f32", 32768), ("bf16", 40001)])
+def test_rows_alike_but_for_two_columns(dtype, M):
+    """p and q have the same ratio at all columns but two; what is left of p - q is some 10^-7 of the row at one of them and as much at all others together, or
+    at that one alone: fp32 sums know neither."""
+    R = _gpu()
+    B, G = 600, 1
+    g = torch.Generator().manual_seed(7)
+    target = block((B, G + 1, M), dtype, 3)
+    cols = torch.stack([torch.randperm(M, generator=g)[:2] for _ in range(B)]).cuda()  # the draft, raised in q; another one, lowered in it
+    low = (torch.randint(-20, 0, (B, 2), generator=g) / 4.0 - 1).cuda()
+    more = (torch.randint(1, 9, (B, 2), generator=g) / 4.0).cuda()
+    target[:, 0].scatter_(1, cols, low.to(target.dtype))
+    draft = target[:, :1].clone()
+    draft[:, 0].scatter_(1, cols, (low + more * torch.tensor([1.0, -1.0], device="cuda")).to(target.dtype))
+    drafts = cols[:, :1].contiguous()
+    u = numbers((B, G + 1), 8)
+    u[:, 0] = 1 - 2.0**-24
+    tokens, accepted = R.rtopk_verify_drafts(target, drafts, u, draft)
+    same((tokens, accepted), by_workgroups(R, target, drafts, u, draft))
+    assert (accepted == 0).all()
+    alone = tokens[:, 0] == cols[:, 1]
+    assert B // 10 < int(alone.sum()) < B - B // 10
+
+
 def test_the_target_as_its_own_draft():
     R = _gpu()
     B, G, M = 300, 2, 20000
