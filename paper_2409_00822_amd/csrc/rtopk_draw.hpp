@@ -759,63 +759,78 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
 
 // With e_p and e_q the powers of two rows about 0, their sums S and l = S_p / S_q, a piece has  sum max(e_p - l e_q, 0) / S_p  of p - q.  That is taken in the pass
 // that finds the sums: about the tests' fp32 ratio k of them, A = sum max(e_p - k e_q, 0) and B = sum of e_q where that is not 0, so that
-// A - (l - k) B is the piece's sum if no column's ratio lies between l and k.  A piece that has a column nearer to k than l may be, k kNearRatio (rows
-// that are alike in most columns have many), is marked, and summed again when l is known.
+// A - (l - k) B is the piece's sum if no column's ratio lies between l and k.  l and k differ by 10^-7 of them or so, and few pieces have such a column, but
+// rows that are alike in most columns have many: the distance of k from the nearest ratio that is nearer than k kNear is kept, and a piece that has one within
+// l - k is summed again when l is known.
 struct Rest {
-  double p, q, a, b;
-  bool near;
+  double p, q, a, b, nearest;
 };
-constexpr int kNearBits = 18;  // l and k differ by 10^-7 to 10^-6 of them; a piece of 2048 columns whose ratios spread over two octaves is marked one time in 200
-constexpr double kNearRatio = 1.0 / (1 << kNearBits);
+constexpr double kNear = 0x1p-16;
 
 template <int DT>
 __device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int cols, int lane, double c, double ratio) {
   using L = Logits<DT>;
-  Rest r = {0.0, 0.0, 0.0, 0.0, false};
+  Rest r = {0.0, 0.0, 0.0, 0.0, __builtin_inf()};
   const int full = cols / L::V, rest = cols % L::V;
-  const double far = ratio * (1 << kNearBits);  // e_q is kept times kNearRatio: what e_p - k e_q is held against
+  const double near = ratio * kNear;
   bool masked = false;
-  const auto add = [&](double ep, double eq, Rest& t) {
-    const double d = __builtin_fma(-far, eq, ep);
+  const auto add = [&](double ep, double eq, Rest& t, bool& close) {
+    const double d = __builtin_fma(-ratio, eq, ep);
     t.p += ep;
     t.q += eq;
     t.a += fmax(d, 0.0);
     t.b += d > 0.0 ? eq : 0.0;
-    t.near |= fabs(d) < ratio * eq;
+    close |= fabs(d) < near * eq;
   };
-  const auto take = [&](float x, float y, Rest& t) { add(power2_finite((double)x * c), power2_finite(__builtin_fma((double)y, c, -(double)kNearBits)), t); };
-  const auto take_masked = [&](float x, float y, Rest& t) {
-    add(masked_power(x, c), power2_finite(y == kNegInf ? -1100.0 : __builtin_fma((double)y, c, -(double)kNearBits)), t);
+  const auto approach = [&](float x, float y) {
+    const double eq = masked_power(y, c), d = __builtin_fma(-ratio, eq, masked_power(x, c));
+    if (fabs(d) < near * eq) r.nearest = fmin(r.nearest, fabs(d) / eq);
   };
   for (int i = lane; i - lane < full; i += 64) {
-    Rest t = {0.0, 0.0, 0.0, 0.0, false};
+    Rest t = {0.0, 0.0, 0.0, 0.0, 0.0};
+    bool close = false;
     u4_vec x[1], y[1];
     if (i < full) {
       x[0] = L::load(p + (int64_t)i * L::V);
       y[0] = L::load(q + (int64_t)i * L::V);
       if (!masked) {
 #pragma unroll
-        for (int k = 0; k < L::V; ++k) take(L::at(x[0], k), L::at(y[0], k), t);
+        for (int k = 0; k < L::V; ++k) add(power2_finite((double)L::at(x[0], k) * c), power2_finite((double)L::at(y[0], k) * c), t, close);
       }
     }
     if (masked || __any(!(t.p + t.q == t.p + t.q))) {  // (-inf, or what is no number)
       masked = true;
-      t = {0.0, 0.0, 0.0, 0.0, false};
+      close = false;
+      t = {0.0, 0.0, 0.0, 0.0, 0.0};
       if (i < full) {
         apart(x);
         apart(y);
 #pragma unroll
-        for (int k = 0; k < L::V; ++k) take_masked(L::at(x[0], k), L::at(y[0], k), t);
+        for (int k = 0; k < L::V; ++k) add(masked_power(L::at(x[0], k), c), masked_power(L::at(y[0], k), c), t, close);
       }
     }
     r.p += t.p;
     r.q += t.q;
     r.a += t.a;
     r.b += t.b;
-    r.near |= t.near;
+    if (__any(close)) {  // (seldom)
+      if (close) {
+#pragma unroll 1
+        for (int k = 0; k < L::V; ++k) approach(L::widen(p[(int64_t)i * L::V + k]), L::widen(q[(int64_t)i * L::V + k]));
+      }
+    }
   }
-  if (lane < rest) take_masked(L::widen(p[full * L::V + lane]), L::widen(q[full * L::V + lane]), r);
-  return {wave_sum(r.p), wave_sum(r.q) * (1 << kNearBits), wave_sum(r.a), wave_sum(r.b) * (1 << kNearBits), (bool)__any(r.near)};
+  if (lane < rest) {
+    const float x = L::widen(p[full * L::V + lane]), y = L::widen(q[full * L::V + lane]);
+    bool close = false;
+    add(masked_power(x, c), masked_power(y, c), r, close);
+    approach(x, y);
+  }
+  if (__any(r.nearest < __builtin_inf())) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) r.nearest = fmin(r.nearest, __shfl_xor(r.nearest, d));
+  }
+  return {wave_sum(r.p), wave_sum(r.q), wave_sum(r.a), wave_sum(r.b), r.nearest};
 }
 
 // S_p / S_q from the tests' fp32 sums.
@@ -846,7 +861,8 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) 
     if (lane == 0) {
       *part = make_double2(0.0, r.p);
       part[a.pieces] = make_double2(0.0, r.q);
-      part[2 * a.pieces] = make_double2(r.a, r.near ? -r.b : r.b);  // (a sign marks it)
+      part[2 * a.pieces] = make_double2(r.a, r.b);
+      a.rest[n * a.pieces + piece] = r.nearest;
     }
   }
 }
@@ -883,14 +899,15 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) 
     w.q = join_mass(draft_part, a.pieces, w.c);
     const double k = near_ratio(a, n, pos, w.c), l = w.p.s / w.q.s;
     const auto in_range = [](double s) { return s >= kLeastSum && s <= kMostSum; };
-    if (in_range(w.p.s) && in_range(w.q.s) && fabs(l - k) < kNearRatio * k) {
+    if (in_range(w.p.s) && in_range(w.q.s) && fabs(l - k) < 0.5 * kNear * k) {
       more = l - k;
       w.over_q = w.q.over();
-      for (int j0 = 0; j0 < a.pieces; j0 += 64) {  // a wavefront takes each W-th piece that is marked
+      const double* nearest = a.rest + n * a.pieces;
+      for (int j0 = 0; j0 < a.pieces; j0 += 64) {  // (each W-th piece is the wavefront's)
         const int mine = j0 + lane;
-        uint64_t marked = __ballot(mine < a.pieces && mine % W == wave && __double_as_longlong(rest[min(mine, a.pieces - 1)].y) < 0);
-        for (; marked != 0; marked &= marked - 1) {
-          const int j = j0 + __builtin_ctzll(marked), first = j * a.piece_cols;
+        uint64_t again = __ballot(mine < a.pieces && mine % W == wave && nearest[min(mine, a.pieces - 1)] <= 1.001 * fabs(more));
+        for (; again != 0; again &= again - 1) {
+          const int j = j0 + __builtin_ctzll(again), first = j * a.piece_cols;
           const double s = piece_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), lane);
           if (lane == 0) rest[j] = make_double2(w.p.s * s, 0.0);
         }

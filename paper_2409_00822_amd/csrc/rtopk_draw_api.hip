@@ -96,9 +96,10 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
     a.groups = l.groups;
     const int64_t rows = rtopk::kept_rows(G, draft, l);
     a.part = static_cast<double2*>(workspace);
+    a.rest = reinterpret_cast<double*>(a.part + B * rows * l.pieces);
     if (l.tested) {
       const int64_t groups = rtopk::ceil_div(l.pieces, rtopk::kDrawWaves);
-      a.near = reinterpret_cast<float2*>(a.part + B * rows * l.pieces);
+      a.near = reinterpret_cast<float2*>(a.rest + B * l.pieces);
       a.accepts = reinterpret_cast<uint8_t*>(a.near + 2 * B * G);
       for (int pos = 0, launch = 0, positions; pos < G; pos += positions, ++launch) {
         positions = l.positions + launch / 2;
@@ -108,7 +109,6 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
       sliced(groups, [&](int64_t n) { return rtopk::launch_draw_rest(dtype, a, n, s); });
       sliced(1, [&](int64_t n) { return rtopk::launch_draw_pick(dtype, a, n, s); });
     } else {
-      a.rest = reinterpret_cast<double*>(a.part + B * rows * l.pieces);
       a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
       sliced(rows * rtopk::ceil_div(l.pieces, rtopk::kDrawWaves), [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
       sliced(l.groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });

@@ -26,7 +26,7 @@ struct DrawArgs {
   // sequences spread over workgroups
   int groups;        // workgroups that draw_join_kernel has for a sequence
   double2* part;     // [B][rows][pieces] masses; tested: [B][3][pieces] of target and draft, and what is left of their difference
-  double* rest;      // [B][pieces] sums of max(p - q, 0)
+  double* rest;      // [B][pieces] sums of max(p - q, 0); tested: how near a column's ratio comes to that of fp32 sums
   int32_t* arrived;  // [B]
   float2* near;      // [B][G][2] (tested) maxima and sums in fp32
   uint8_t* accepts;  // [B][G] (tested) what has been accepted

@@ -88,11 +88,11 @@ inline DrawLayout draw_layout(int64_t B, int G, int M, int dtype, bool draft) {
   return l;
 }
 
-// Device memory: the pieces' results; untested their sums of max(p - q, 0) and a counter for each sequence; tested the drafts' fp32 sums and what is accepted.
+// Device memory: the pieces' results; a number for each; untested a counter for each sequence; tested the drafts' fp32 sums and what is accepted.
 inline int64_t draw_workspace(int64_t B, int G, bool draft, const DrawLayout& l) {
   if (!l.spread) return 0;
   const int64_t parts = B * l.pieces * 16 * (int64_t)kept_rows(G, draft, l);
-  return l.tested ? parts + 17 * B * G : parts + 8 * B * l.pieces + 4 * B;
+  return parts + 8 * B * l.pieces + (l.tested ? 17 * B * G : 4 * B);
 }
 
 }  // namespace rtopk
