@@ -15,6 +15,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "rtopk_draw_dispatch.hpp"
 #include "rtopk_logits.hpp"
 
@@ -159,12 +161,28 @@ __device__ __forceinline__ Mass piece_mass(const typename Logits<DT>::elem* piec
   return t;
 }
 
+// f(0), ..., f(n - 1) of memory, one to a lane, 64 at a time: the first 128 are held in registers, for all loops over them.
+template <typename F>
+struct Held {
+  using T = decltype(std::declval<F>()(0));
+  int n;
+  F f;
+  T v[2];
+  __device__ __forceinline__ Held(int n, F f) : n(n), f(f), v{} {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if ((int)(threadIdx.x & 63) + 64 * i < n) v[i] = f((int)(threadIdx.x & 63) + 64 * i);
+  }
+  __device__ __forceinline__ T at(int j) const { return j < 64 ? v[0] : (j < 128 ? v[1] : f(j)); }  // j: the lane's, below n
+};
+
 // A row's mass from its pieces' (ref, s), in every lane; each wavefront for itself.
-__device__ __forceinline__ Mass join_mass(const double2* part, int pieces, double c) {
+template <typename H>
+__device__ __forceinline__ Mass join_held(const H& part, double c) {
   const int lane = threadIdx.x & 63;
   Mass t = {0.0, 0.0};
-  for (int j = lane; j < pieces; j += 64) {
-    const double2 p = part[j];
+  for (int j = lane; j < part.n; j += 64) {
+    const double2 p = part.at(j);
     if (p.y != 0.0) {  // (NaN too)
       const double ref = t.s == 0.0 ? p.x : fmax(t.ref, p.x);
       if (ref != t.ref && t.s != 0.0) t.s *= power2((t.ref - ref) * c);
@@ -182,6 +200,9 @@ __device__ __forceinline__ Mass join_mass(const double2* part, int pieces, doubl
     if (t.s != 0.0 && t.ref != ref) t.s *= power2((t.ref - ref) * c);
   }
   return {ref, wave_sum(t.s)};
+}
+__device__ __forceinline__ Mass join_mass(const double2* part, int pieces, double c) {
+  return join_held(Held(pieces, [=](int j) { return part[j]; }), c);
 }
 
 // Temperature 0: place_key of the largest logit, 0 where there is none, and whether there is a NaN.
@@ -394,37 +415,57 @@ __device__ int block_find(const Weights& w, const typename Logits<DT>::elem* p, 
   return at;
 }
 
-// A draw by u from the weights of a row: rest(j) are its pieces' sums where they are p - q, else part[j] their masses in p.  Draws from p where the weights'
-// whole is no more than kLeastMass.
-template <int DT, int W, typename R>
-__device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, const double2* part, R rest, double u,
-                          FindRoom<W>& room) {
+// A draw by u from the weights of a row, sum(j) its pieces' sums of them; -2: their whole is no more than `least`.
+template <int DT, int W, typename S>
+__device__ __forceinline__ int block_draw_of(const DrawArgs& a, const Weights& w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, S sum, double u, double least,
+                                             FindRoom<W>& room) {
   const int lane = threadIdx.x & 63;
-  const auto cols = [&](int j) { return min(a.piece_cols, a.M - j * a.piece_cols); };
-  // the piece with the draft that stood for itself, without it; each wavefront for itself
-  const int special = w.without >= 0 ? w.without / a.piece_cols : -1;
-  const double special_sum = special >= 0 ? piece_weight<DT>(w, p, q, special * a.piece_cols, cols(special), lane) : 0.0;
-  for (;;) {
-    const auto sum = [&](int j) {
-      if (w.less) return rest(j);
-      if (w.without >= 0 && j == special) return special_sum;
-      const double2 t = part[j];
-      return t.y * (t.x == w.p.ref || t.y == 0.0 ? 1.0 : power2((t.x - w.p.ref) * w.c)) * w.over_p;
-    };
-    double all = 0.0;
-    for (int j = lane; j < a.pieces; j += 64) all += sum(j);
-    all = wave_sum(all);
-    if ((w.less || w.without >= 0) && !(all > kLeastMass)) {
-      w.less = false;
-      w.without = -1;
-      continue;
+  const Held held(a.pieces, sum);
+  double all = 0.0;
+  for (int j = lane; j < a.pieces; j += 64) all += held.at(j);
+  all = wave_sum(all);
+  if (!(all > least)) return -2;
+  const double goal = fmax(u * all, 0.0);  // (NaN: 0)
+  double before = 0.0;
+  const int j = passing(a.pieces, goal, before, [&](int i) { return held.at(i); });
+  return j < 0 ? -1 : block_find<DT, W>(w, p, q, j * a.piece_cols, min(a.piece_cols, a.M - j * a.piece_cols), before, goal, room);
+}
+
+// What a piece with mass t weighs in p.
+__device__ __forceinline__ double weight_of(const Weights& w, const double2& t) {
+  return t.y * (t.x == w.p.ref || t.y == 0.0 ? 1.0 : power2((t.x - w.p.ref) * w.c)) * w.over_p;
+}
+
+// A draw from the weights of a row: rest(j) are its pieces' sums where they are p - q, else part(j) their masses in p.  Draws from p where the weights' whole is
+// no more than kLeastMass.
+template <int DT, int W, typename P, typename R>
+__device__ int block_draw(const DrawArgs& a, Weights w, const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, P part, R rest, double u, FindRoom<W>& room) {
+  int at = -2;
+  if (w.less) {
+    at = block_draw_of<DT, W>(a, w, p, q, rest, u, kLeastMass, room);
+  } else if (w.without >= 0) {
+    // the piece with the draft that stood for itself, without it
+    const int special = w.without / a.piece_cols, first = special * a.piece_cols, wave = threadIdx.x >> 6;
+    double s = 0.0;
+    each_weight<DT>(w, p, q, first, min(a.piece_cols, a.M - first), threadIdx.x, 64 * W, [&](const double(&v)[Logits<DT>::V], int) {
+#pragma unroll
+      for (int c = 0; c < Logits<DT>::V; ++c) s += v[c];
+    });
+    s = wave_sum(s);
+    if (W > 1) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) room.s[wave] = s;
+      __syncthreads();
+      s = 0.0;
+#pragma unroll
+      for (int i = 0; i < W; ++i) s += room.s[i];
     }
-    if (!(all > 0.0)) return -1;
-    const double goal = fmax(u * all, 0.0);  // (NaN: 0)
-    double before = 0.0;
-    const int j = passing(a.pieces, goal, before, sum);
-    return j < 0 ? -1 : block_find<DT, W>(w, p, q, j * a.piece_cols, cols(j), before, goal, room);
+    at = block_draw_of<DT, W>(a, w, p, q, [&](int j) { return j == special ? s : weight_of(w, part(j)); }, u, kLeastMass, room);
   }
+  if (at != -2) return at;
+  w.less = false;
+  w.without = -1;
+  return max(block_draw_of<DT, W>(a, w, p, q, [&](int j) { return weight_of(w, part(j)); }, u, 0.0, room), -1);
 }
 
 // ---- sequences ------------------------------------------------------------------------------------
@@ -541,7 +582,7 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
         });
         __syncthreads();
       }
-      drawn = block_draw<DT, W>(a, w, p, q, part, [&](int j) { return rest[j]; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+      drawn = block_draw<DT, W>(a, w, p, q, [&](int j) { return part[j]; }, [&](int j) { return rest[j]; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
     }
   }
   write_sequence(a, n, pos, drawn, 64 * W);
@@ -643,6 +684,36 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) 
     out = make_double2(t.ref, t.s);
   }
   if (lane == 0) a.part[(n * rows + row) * a.pieces + piece] = out;
+}
+
+// The draws of sequences without drafts from their masses.
+template <int DT, int W>
+__global__ __launch_bounds__(64 * W) void draw_take_kernel(DrawArgs a) {
+  __shared__ FindRoom<W> room;
+  const int64_t n = a.row0 + blockIdx.x;
+  const Heat heat(a, n);
+  const double2* part = a.part + n * a.pieces;
+  int drawn = -1;
+  if (heat.certain()) {
+    drawn = join_best(part, a.pieces).col();
+  } else if (!heat.none()) {
+    const double u = (double)a.uniforms[n];
+    const Held held(a.pieces, [=](int j) { return part[j]; });
+    Weights w;
+    w.c = heat.c;
+    w.p = w.q = join_held(held, w.c);
+    w.over_p = w.over_q = w.p.over();
+    w.without = -1;
+    w.less = false;
+    if (w.is_number()) {
+      const auto* p = row_of<DT>(a, n, 0);
+      drawn = max(block_draw_of<DT, W>(a, w, p, p, [&](int j) { return weight_of(w, held.at(j)); }, u, 0.0, room), -1);
+    }
+  }
+  if (threadIdx.x == 0) {
+    write_token(a, n, drawn);
+    if (a.accepted) a.accepted[n] = 0;
+  }
 }
 
 // Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
@@ -749,8 +820,9 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
     __syncthreads();
     if (!last) return;
   }
+  const double2* part = parts + (int64_t)pos * a.pieces;
   const int drawn = block_draw<DT, W>(
-      a, w, p, q, parts + (int64_t)pos * a.pieces, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
+      a, w, p, q, [&](int j) { return part[j]; }, [&](int j) { return __hip_atomic_load(rest + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
       (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }
@@ -941,7 +1013,7 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) 
   }
   int drawn = -1;
   if (w.is_number())
-    drawn = block_draw<DT, W>(a, w, p, q, part, [&](int j) { return fmax(__builtin_fma(-more, rest[j].y, rest[j].x), 0.0) * w.over_p; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+    drawn = block_draw<DT, W>(a, w, p, q, [&](int j) { return part[j]; }, [&](int j) { return fmax(__builtin_fma(-more, rest[j].y, rest[j].x), 0.0) * w.over_p; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }
 

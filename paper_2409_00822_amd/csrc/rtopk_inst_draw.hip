@@ -40,6 +40,7 @@ hipError_t pick_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
 
 template <int DT>
 hipError_t join_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
+  if (a.G == 0) return launch_kernel(draw_take_kernel<DT, kDrawWaves>, dim3((uint32_t)n), dim3(64 * kDrawWaves), 0, s, a);
   return launch_kernel(draw_join_kernel<DT, kDrawWaves>, dim3((uint32_t)(n * a.groups)), dim3(64 * kDrawWaves), 0, s, a);
 }
 
