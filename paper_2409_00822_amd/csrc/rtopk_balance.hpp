@@ -584,7 +584,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
       const float* value = pv + (VALS ? u * PER * a.k : 0);
       col[u] = pick_of(a, col[u]);
       uint64_t ballot = __ballot(col[u] >= 0);
-      bool once = true;  // picks that ascend, so that none is there twice
+      bool left_out = false, once = true;  // picks that ascend, so that none is there twice
       if (VALS) {
         const int before = __builtin_amdgcn_update_dpp(0, col[u], 0x138, 0xf, 0xf, false);  // wave_shr:1
         once = !__any(col[u] >= 0 && sub > 0 && !(before >= 0 && before < col[u]));
@@ -598,7 +598,8 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
             once = once && !__any(mine >= 0 && !(before >= 0 && before < mine));
           }
         }
-        R::leave_out(!any_lane<N>(ballot, of), raw[u]);
+        left_out = !any_lane<N>(ballot, of);
+        R::leave_out(left_out, raw[u]);
       }
       const RouterRow<DT, N, LOADS, RAGGED> row(r, raw[u]);
       // f(column, the gradients that it gets) for the picks of the lane, but for the first where there is one to a column
@@ -649,6 +650,10 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void balance_grad_kernel(Balanc
         for (int c = 0; c < V; ++c) {
           const float t = __builtin_fmaf(w[i][c], over, both);
           d[c] = VALS ? __builtin_fmaf(row.e[i][c], t, v[c]) : row.e[i][c] * t;
+        }
+        if (__any(left_out)) {  // (0, whatever the group's gradients are)
+#pragma unroll
+          for (int c = 0; c < V; ++c) d[c] = left_out ? 0.0f : d[c];
         }
         if (is && r.has[i]) {
           auto* at = to + u * PER * a.grad_stride + r.at[i];

@@ -197,6 +197,43 @@ def test_tokens_left_out_and_groups_of_padding():
     assert (grad[:20] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_tokens_left_out_of_a_loss_that_overflowed(dtype):
+    """Padding has a gradient of 0 also where a loss scale has made the group's gradients infinite."""
+    R = _gpu()
+    x, cols = inputs(400, 24, 3, dtype, 1, ignored=4)
+    _, _, _, counts, rows = R.rtopk_balance_loss(x, cols, 4)
+    out = (cols < 0).all(1)
+    bad = torch.tensor([float("inf"), float("nan"), -float("inf"), 1.0], device="cuda")
+    for gz, vals in ((None, None), (bad.flip(0).contiguous(), torch.ones((400, 3), device="cuda"))):
+        grad = R.rtopk_balance_loss_backward(bad, x, cols, counts, rows, gz, vals)
+        assert out.sum() == 100 and (grad[out] == 0).all() and not grad[:100][~out[:100]].isfinite().any()
+
+
+def test_offsets_beyond_32_bits():
+    """The last of two groups of 2^32 logits each behind the other."""
+    R = _gpu()
+    N, E, k = 1 << 25, 256, 2
+    x = torch.zeros((N, E), dtype=torch.bfloat16, device="cuda")
+    cols = torch.zeros((N, k), dtype=torch.int32, device="cuda")
+    cols[:, 1] = 1
+    tail, picked = inputs(N // 2 // 64, E, k, "bf16", 3)
+    for i in range(64):
+        x[N // 2 + i * tail.shape[0]:][:tail.shape[0]] = tail
+        cols[N // 2 + i * tail.shape[0]:][:tail.shape[0]] = picked
+    whole = R.rtopk_balance_loss(x, cols, 2)
+    assert whole[3][0].tolist() == [N // 2, N // 2] + [0] * (E - 2) and whole[4].tolist() == [N // 2] * 2
+    assert torch.equal(whole[3][1], 64 * R.rtopk_balance_loss(tail, picked)[3][0])
+    near(wide(whole[0][:1]), [1.0], 200 * U, "loss")  # (equal probabilities, 1 / E each: f_e P_e E sums to 1)
+    few = R.rtopk_balance_loss(tail, picked)
+    near(wide(whole[0][1:]), wide(few[0]), 240 * U * wide(few[0]), "loss")  # (each within (2 D + 80) U of the definition, as above, D < 20)
+    grad = torch.ones((2,), device="cuda") * N
+    got = R.rtopk_balance_loss_backward(grad, x, cols, whole[3], whole[4], None, None, x)
+    last = R.rtopk_balance_loss_backward(grad[1:], tail, picked, whole[3][1:], whole[4][1:])
+    assert torch.equal(got[-tail.shape[0]:], last) and not got[N // 2:].isnan().any()
+    assert torch.equal(got[0], got[N // 2 - 1])
+
+
 def test_no_tokens():
     R = _gpu()
     x, cols = torch.empty((0, 8), device="cuda"), torch.empty((0, 2), dtype=torch.int32, device="cuda")

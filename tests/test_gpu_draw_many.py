@@ -203,6 +203,28 @@ def test_rows_that_end_with_their_allocation(dtype, N, M):
     assert torch.equal(got[-3:], R.rtopk_sample_tokens(x[-3:], u[-3:].contiguous()))
 
 
+def test_offsets_beyond_32_bits():
+    R = _gpu()
+    # rows: one behind the other, and far apart
+    N, M = 66000, 65536
+    x = torch.full((N, M), -float("inf"), dtype=torch.bfloat16, device="cuda")
+    x[-5:] = block((5, M), "bf16", 1)
+    u = numbers((N,), 1)
+    got = R.rtopk_sample_tokens(x, u)
+    assert (got[:-5] == -1).all()
+    assert torch.equal(got[-5:], check_sample(R, x[-5:], u[-5:].contiguous(), 1.0))
+    # sequences
+    flat = x.view(-1)
+    for B, G, M, seq, pos in ((2, 2, 40000, 1 << 31, 1 << 29), (512, 1, 16500, (1 << 23) + 8, 1 << 22), (2, 1, 700, (1 << 32) - (1 << 29), 1 << 28)):
+        assert (B - 1) * seq + G * pos + M <= flat.numel()
+        target = torch.as_strided(flat, (B, G + 1, M), (seq, pos, 1))
+        target.copy_(block((B, G + 1, M), "bf16", 2))
+        draft = torch.as_strided(flat, (B, G, M), (seq, pos, 1), M + 3)
+        draft.copy_(near_draft(target, G, 3))
+        drafts, u = drawn_from(draft, 1.0, 4), numbers((B, G + 1), 5)
+        same(R.rtopk_verify_drafts(target, drafts, u, draft), R.rtopk_verify_drafts(target.contiguous(), drafts, u, draft.contiguous()))
+
+
 def test_decoding_with_drafts():
     """A target and a draft model (a table of logits by the last token) that decode together.  At temperature 0 the text is the target's own; with random numbers the drafted
     calls are those of the definitions."""
