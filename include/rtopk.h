@@ -281,7 +281,7 @@ int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dt
 /*
  * Tokens drawn from rows of logits, and drafted tokens verified
  * --------------------------------------------------------------
- * Random numbers are inputs, and a result is a pure function of its inputs: differences, powers and sums are 64-bit, taken in an order that
+ * Random numbers are inputs, and a result is a pure function of its inputs: what decides on a token is computed in 64 bits, in an order that
  * depends on the call's sizes only.  A row x at temperature T has probabilities p_v = exp((x_v - max x) / T) / sum; at T = 0 all of it is on the largest logit, the
  * lowest column of equal ones.  By a number u in [0, 1) it gives the lowest column v with  p_0 + ... + p_v > u  (u below 0 or NaN counts as 0; where rounding or
  * u >= 1 leaves none, the last column with p_v > 0).  A row without a distribution -- nothing but -inf, or with a NaN, or with +inf at T > 0 -- gives -1.
@@ -308,8 +308,8 @@ int rtopk_sample_tokens(const void* logits, int32_t dtype, int64_t N, int32_t M,
  * as if drawn from the target one by one, if the drafts were drawn from q.
  *   target_logits : [B][G + 1][M], sequences target_seq_stride and their rows target_pos_stride elements apart, each >= M, in any order.
  *   draft_logits  : [B][G][M] of the same type, likewise; NULL: a draft stands for itself, q_i(d_i) = 1 (as where T is 0).  A row of nothing but -inf has q = 0.
- *   drafts        : [B][G], 0 <= G <= 128.  The first token outside [0, M) ends a sequence's drafts; rows behind the one that the last token is drawn from are not
- *                   looked at.
+ *   drafts        : [B][G], 0 <= G <= 128.  The first token outside [0, M) ends a sequence's drafts; nothing depends on rows behind the one that the last token is
+ *                   drawn from.
  *   uniforms      : [B][G + 1].
  *   out_tokens    : [B][G + 1]: the accepted drafts, the drawn token, -1 behind it.     out_accepted : [B] int32_t, how many were accepted (optional).
  */

@@ -52,10 +52,12 @@ inline DrawLayout draw_layout_whole(int64_t B, int M, int dtype) {
 
 // One workgroup to a sequence, us against spread ones: tokens of rows of up to 8192 columns (1 x 8000 bfloat16 7.8 and 8.8, 1024 x 4000 11.7 and 13.2; 64 x 32000 15.1 and
 // 10.6, 4096 x 32000 130 and 107); drafts where rows are short and few (256 sequences of one draft, 1000 columns 10.2 and 13.5, 4000 12.1 and 16.5; of four
-// drafts 20.1 and 16.5) or sequences many (4096 of four drafts, 1000 columns 56 and 98).
+// drafts 20.1 and 16.5) or sequences many (4096 of four drafts, 1000 columns 56 and 98).  Very many sequences: tokens of 16385 rows of 12000 columns 248 and 233, 32000
+// 562 and 520, 131072 1444 and 1543, so that scratch memory is spared; drafts are tested first, which pays (16385 of four drafts, 32000 columns 2686
+// and 1775, three of 8000 713 and 555).
 inline bool by_workgroups(int64_t B, int G, int M) {
-  if (B > 16384) return true;
-  if (G == 0) return M <= 8192;
+  if (G == 0) return M <= 8192 || B > 16384;
+  if (M > kMostTested && B >= 512) return true;
   return G <= 2 ? M <= 4096 : (M <= 2048 && B >= 1024);
 }
 

@@ -310,6 +310,20 @@ def test_with_and_without_scratch_memory(B, G, M):
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("dtype,B,G,M", [("bf16", 2, 0, 1 << 24), ("f32", 1, 0, (1 << 24) - 5), ("f16", 1, 1, 3000001), ("bf16", 3, 1, 1200000)])
+def test_the_widest_rows(dtype, B, G, M):
+    R = _gpu()
+    lib = R.load_library()
+    target, u = block((B, G + 1, M), dtype, 3), numbers((B, G + 1), 4)
+    draft = (target[:, :G].float() + 0.5 * block((B, G, M), "f32", 2)).to(TYPES[dtype]) if G else None
+    drafts = draft.argmax(-1) if G else torch.zeros((B, 0), dtype=torch.int64, device="cuda")
+    want = check_verify(R, target, drafts, u, draft)
+    out, n = torch.empty_like(want[0]), torch.empty_like(want[1])
+    status = lib.rtopk_verify_drafts(target.data_ptr(), draft.data_ptr() if G else None, list(TYPES).index(dtype), B, G, M, (G + 1) * M, M, G * M, M, drafts.data_ptr() if G else None, 8, u.data_ptr(),
+                                     None, 1.0, out.data_ptr(), n.data_ptr(), None, 0, torch.cuda.current_stream().cuda_stream)
+    assert status == 0 and torch.equal(out, want[0]) and torch.equal(n, want[1])
+
+
 def test_captured_and_on_other_streams():
     R = _gpu()
     B, G, M = 4, 3, 32000
