@@ -629,8 +629,8 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
     const double u = (double)a.uniforms[n * (a.G + 1) + pos];
     const float c = (float)heat.c;
     const auto near = [&](const elem* x, int which) {
-      const Segment<DT> g(x, a.M);
-      const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, 4, false, false>(g, c), c, sums);
+      const Segment<DT> g(x, a.M);  // (eight loads at a time for a workgroup of sixteen, which has no other beside it)
+      const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, W == 16 ? 8 : 4, false, false>(g, c), c, sums);
       __syncthreads();
       if (threadIdx.x == 0) a.near[2 * (n * a.G + pos) + which] = make_float2(t.m, t.s);
       return power2(((double)Logits<DT>::widen(x[d]) - (double)t.m) * heat.c) / (double)t.s;

@@ -81,8 +81,9 @@ inline DrawLayout draw_layout(int64_t B, int G, int M, int dtype, bool draft) {
   if (tested) {
     l.tested = true;
     l.positions = (int)(B < 512 ? ceil_div(512, B) : 1);
-    const int64_t workgroups = B * l.positions;
-    l.test_waves = workgroups <= 256 ? 16 : (workgroups <= 512 ? 8 : 4);
+    const int64_t workgroups = B * (l.positions < G ? l.positions : G);
+    // sixteen for rows of at least their first loads (160 workgroups, rows of 256 KiB 17.6 us and 20.8 with eight; 192, of 98 KiB 8.2 and 7.8)
+    l.test_waves = workgroups <= 256 && M >= 16 * 8 * 64 * logits_width(dtype) ? 16 : (workgroups <= 512 ? 8 : 4);
   } else if (draft) {
     l.groups = (int)ceil_div(l.pieces, kDrawWaves);
     if (B * l.groups > 1024) l.groups = B < 1024 ? (int)(1024 / B) : 1;
