@@ -55,7 +55,7 @@ __device__ __forceinline__ double masked_power(float x, double c) { return power
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double moved(double v) {
   const long long b = __double_as_longlong(v);
-  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, ROWS == 0xf), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, ROWS == 0xf);
   return __longlong_as_double((long long)hi << 32 | (uint32_t)lo);
 }
 __device__ __forceinline__ double lane_value(double v, int lane) {  // lane: uniform
@@ -130,24 +130,23 @@ template <int DT>
 __device__ __forceinline__ Mass piece_mass(const typename Logits<DT>::elem* piece, int cols, int lane, double c) {
   using L = Logits<DT>;
   constexpr int U = DT == kF32 ? 4 : 2;
-  const Segment<DT> g(piece, cols);
+  const int full = cols / L::V, rest = cols % L::V;
   double s = 0.0;
   bool masked = false;
   int i = lane;
-  for (; i - lane + U * 64 <= g.full; i += U * 64) {
+  for (; i - lane + U * 64 <= full; i += U * 64) {
     u4_vec w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = L::load(g.body + (uint32_t)(i + u * 64) * L::V);
+    for (int u = 0; u < U; ++u) w[u] = L::load(piece + (uint32_t)(i + u * 64) * L::V);
     s += chunk_powers<DT, U>(w, c, masked);
   }
-  for (; i - lane < g.chunks(); i += 64) {
+  for (; i - lane < full; i += 64) {
     u4_vec w[1] = {u4_vec{L::kLow, L::kLow, L::kLow, L::kLow}};
-    const int kind = chunk_kind(i, g.full, g.rest + g.lead);
-    if (kind == kWholeChunk) w[0] = L::load(g.body + (uint32_t)i * L::V);
-    else if (kind == kPartialChunk) w[0] = g.partial();
-    masked |= i - lane + 64 > g.full;
+    if (i < full) w[0] = L::load(piece + (uint32_t)i * L::V);
+    masked |= i - lane + 64 > full;
     s += chunk_powers<DT, 1>(w, c, masked);
   }
+  if (lane < rest) s += masked_power(L::widen(piece[full * L::V + lane]), c);
   Mass t = {0.0, wave_sum(s)};
   if (!(t.s >= kLeastSum && t.s <= kMostSum)) {  // about the maximum then
     float m = kNegInf;
@@ -663,10 +662,10 @@ __device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.draft ? 2 *
 // rejected draft among them: few sequences leave the GPU room for that.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) {
-  const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves, of = blockIdx.x / groups, rows = (uint32_t)rows_of(a);
-  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, row = (int)(of % rows);
-  const int64_t n = a.row0 + of / rows;
-  if (blockIdx.x % groups == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
+  const uint32_t rows = (uint32_t)rows_of(a);
+  const int piece = (int)blockIdx.x * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, row = rows == 1 ? 0 : (int)(blockIdx.y % rows);
+  const int64_t n = a.row0 + (rows == 1 ? blockIdx.y : blockIdx.y / rows);
+  if (blockIdx.x == 0 && row == 0 && threadIdx.x == 0) a.arrived[n] = 0;
   if (piece >= a.pieces) return;
   const Heat heat(a, n);
   if (heat.none() || (heat.certain() && row > a.G)) return;
@@ -914,9 +913,8 @@ __device__ __forceinline__ double near_ratio(const DrawArgs& a, int64_t n, int p
 // The pieces of the row that a sequence draws from, one to a wavefront: its mass, and that of the draft's row and what is left of p - q where a draft was rejected.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) {
-  const uint32_t groups = (uint32_t)(a.pieces + kDrawWaves - 1) / kDrawWaves;
-  const int piece = (int)(blockIdx.x % groups) * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t n = a.row0 + blockIdx.x / groups;
+  const int piece = (int)blockIdx.x * kDrawWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t n = a.row0 + blockIdx.y;
   const Heat heat(a, n);
   if (piece >= a.pieces || heat.none()) return;
   const int g = drafts_of(a, n), pos = tested_up_to(a, n, g), first = piece * a.piece_cols, cols = min(a.piece_cols, a.M - first);

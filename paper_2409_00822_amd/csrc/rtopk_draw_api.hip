@@ -87,9 +87,10 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
   a.pieces = l.pieces;
   a.piece_cols = l.cols;
   hipError_t err = hipSuccess;
-  // launch(sequences) for slices whose workgroups fit one launch (2^31 threads)
-  const auto sliced = [&](int64_t each, auto launch) {
-    const int64_t most = (1 << 21) / each;
+  // launch(sequences) for slices whose workgroups fit one launch: 2^31 threads, 65535 rows of a grid with `rows` to a sequence (0: without)
+  const auto sliced = [&](int64_t each, int64_t rows, auto launch) {
+    int64_t most = (1 << 21) / each;
+    if (rows > 0 && most > 65535 / rows) most = 65535 / rows;
     for (a.row0 = 0; a.row0 < B && err == hipSuccess; a.row0 += most) err = launch(B - a.row0 < most ? B - a.row0 : most);
   };
   if (l.spread) {
@@ -104,17 +105,17 @@ int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int
       for (int pos = 0, launch = 0, positions; pos < G; pos += positions, ++launch) {
         positions = l.positions + launch / 2;
         if (positions > G - pos) positions = G - pos;
-        sliced(positions, [&](int64_t n) { return rtopk::launch_draw_test(dtype, l.test_waves, a, pos, positions, n, s); });
+        sliced(positions, 0, [&](int64_t n) { return rtopk::launch_draw_test(dtype, l.test_waves, a, pos, positions, n, s); });
       }
-      sliced(groups, [&](int64_t n) { return rtopk::launch_draw_rest(dtype, a, n, s); });
-      sliced(1, [&](int64_t n) { return rtopk::launch_draw_pick(dtype, a, n, s); });
+      sliced(groups, 1, [&](int64_t n) { return rtopk::launch_draw_rest(dtype, a, n, s); });
+      sliced(1, 0, [&](int64_t n) { return rtopk::launch_draw_pick(dtype, a, n, s); });
     } else {
       a.arrived = reinterpret_cast<int32_t*>(a.rest + B * l.pieces);
-      sliced(rows * rtopk::ceil_div(l.pieces, rtopk::kDrawWaves), [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
-      sliced(l.groups, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
+      sliced(rows * rtopk::ceil_div(l.pieces, rtopk::kDrawWaves), rows, [&](int64_t n) { return rtopk::launch_draw_mass(dtype, a, n, s); });
+      sliced(l.groups, 0, [&](int64_t n) { return rtopk::launch_draw_join(dtype, a, n, s); });
     }
   } else {
-    sliced(1, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
+    sliced(1, 0, [&](int64_t n) { return rtopk::launch_draw(dtype, l.waves, a, n, s); });
   }
   return err == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;
 }

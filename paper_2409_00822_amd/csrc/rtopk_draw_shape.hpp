@@ -10,10 +10,6 @@ namespace rtopk {
 
 constexpr int kMaxDrafts = 128;  // drafted tokens of a sequence
 
-// What chunk i of a piece is that has `full` whole ones and `left` columns beside them.
-enum ChunkKind { kNoChunk = 0, kWholeChunk = 1, kPartialChunk = 2 };
-constexpr int chunk_kind(int i, int full, int left) { return i < full ? kWholeChunk : (i == full && left != 0 ? kPartialChunk : kNoChunk); }
-
 constexpr int kDrawWaves = 4;    // of a workgroup that shares a sequence with others
 constexpr int kMostPieces = 64;  // of a row that one workgroup takes
 constexpr int kMostTested = 1 << 20;  // columns of rows that are tested in fp32: the sums' errors are bounded for that many

@@ -25,12 +25,12 @@ hipError_t test_of_type(int waves, const DrawArgs& a, int pos0, int positions, i
 template <int DT>
 hipError_t mass_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
   const int64_t rows = draw_rows(a.G, a.draft != nullptr);
-  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)(n * rows * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
+  return launch_kernel(draw_mass_kernel<DT>, dim3((uint32_t)ceil_div(a.pieces, kDrawWaves), (uint32_t)(n * rows)), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 template <int DT>
 hipError_t rest_of_type(const DrawArgs& a, int64_t n, hipStream_t s) {
-  return launch_kernel(draw_rest_kernel<DT>, dim3((uint32_t)(n * ceil_div(a.pieces, kDrawWaves))), dim3(64 * kDrawWaves), 0, s, a);
+  return launch_kernel(draw_rest_kernel<DT>, dim3((uint32_t)ceil_div(a.pieces, kDrawWaves), (uint32_t)n), dim3(64 * kDrawWaves), 0, s, a);
 }
 
 template <int DT>

@@ -126,34 +126,25 @@ def test_hand_traces():
 
 CHUNKS = r"""
 #include <stdio.h>
-#include "rtopk_draw_shape.hpp"
-using namespace rtopk;
 // The columns that the lanes of a wavefront read of a piece (piece_mass): each of the piece once, none beyond it.
 int main() {
   long bad = 0;
   for (int V = 4; V <= 8; V += 4)
-    for (int lead = 0; lead <= (V == 8); ++lead)
-      for (int cols = 1; cols <= 4096; ++cols) {
-        static int seen[4200];
-        for (int c = 0; c < 4200; ++c) seen[c] = 0;
-        const int full = (cols - lead) / V, rest = (cols - lead) % V, chunks = full + (rest + lead != 0), U = V == 4 ? 4 : 2;
-        for (int lane = 0; lane < 64; ++lane) {
-          int i = lane;
-          const auto whole = [&](int chunk) { for (int c = 0; c < V; ++c) ++seen[lead + chunk * V + c]; };
-          for (; i - lane + U * 64 <= full; i += U * 64)
-            for (int u = 0; u < U; ++u) whole(i + u * 64);
-          for (; i - lane < chunks; i += 64) {
-            const int kind = chunk_kind(i, full, rest + lead);
-            if (kind == kWholeChunk) whole(i);
-            if (kind == kPartialChunk) {
-              if (rest + lead == 0) ++bad;  // its loads for columns that it has not go to one that it has
-              for (int c = 0; c < rest; ++c) ++seen[lead + full * V + c];
-              if (lead) ++seen[0];
-            }
-          }
-        }
-        for (int c = 0; c < 4200; ++c) bad += seen[c] != (c < cols);
+    for (int cols = 1; cols <= 4096; ++cols) {
+      static int seen[4200];
+      for (int c = 0; c < 4200; ++c) seen[c] = 0;
+      const int full = cols / V, rest = cols % V, U = V == 4 ? 4 : 2;
+      for (int lane = 0; lane < 64; ++lane) {
+        int i = lane;
+        const auto whole = [&](int chunk) { for (int c = 0; c < V; ++c) ++seen[chunk * V + c]; };
+        for (; i - lane + U * 64 <= full; i += U * 64)
+          for (int u = 0; u < U; ++u) whole(i + u * 64);
+        for (; i - lane < full; i += 64)
+          if (i < full) whole(i);
+        if (lane < rest) ++seen[full * V + lane];
       }
+      for (int c = 0; c < 4200; ++c) bad += seen[c] != (c < cols);
+    }
   printf("%ld\n", bad);
   return bad != 0;
 }

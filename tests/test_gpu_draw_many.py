@@ -225,6 +225,20 @@ def test_offsets_beyond_32_bits():
         same(R.rtopk_verify_drafts(target, drafts, u, draft), R.rtopk_verify_drafts(target.contiguous(), drafts, u, draft.contiguous()))
 
 
+def test_more_sequences_than_a_launch_has():
+    R = _gpu()
+    B, G, M = 66000, 1, 4100
+    torch.manual_seed(5)
+    target = torch.empty((B, G + 1, M), dtype=torch.bfloat16, device="cuda").normal_().mul_(3)
+    draft = target[:, :G] + torch.empty((B, G, M), dtype=torch.bfloat16, device="cuda").normal_()
+    drafts, u = draft.argmax(-1), numbers((B, G + 1), 5)
+    got = R.rtopk_verify_drafts(target, drafts, u, draft)
+    same(got, by_workgroups(R, target, drafts, u, draft))
+    last = slice(B - 600, B)
+    check_verify(R, target[last], drafts[last], u[last], draft[last])
+    assert torch.equal(got[0][last], R.rtopk_verify_drafts(target[last], drafts[last], u[last], draft[last])[0])
+
+
 def test_decoding_with_drafts():
     """A target and a draft model (a table of logits by the last token) that decode together.  At temperature 0 the text is the target's own; with random numbers the drafted
     calls are those of the definitions."""
