@@ -41,7 +41,7 @@ extern "C" {
 
 int64_t rtopk_balance_workspace_bytes(int64_t N, int32_t E, int32_t dtype, int32_t k, int32_t groups) {
   if (N < 1 || E < 1 || k < 1 || k > E || E > rtopk::kMaxExperts || !is_type(dtype) || groups < 1 || groups > rtopk::kMaxBalanceGroups || N % groups != 0) return 0;
-  return rtopk::balance_workspace(groups, E, rtopk::balance_layout(groups, N / groups, E, dtype, k, true));
+  return rtopk::balance_workspace(groups, E, rtopk::balance_layout(groups, N / groups, rtopk::router_lanes(E, dtype, k, false), true));
 }
 
 int rtopk_balance_loss(const void* logits, int32_t dtype, int64_t N, int32_t E, int64_t stride, const void* cols, int32_t col_bytes, int32_t k,
@@ -66,8 +66,9 @@ int rtopk_balance_loss(const void* logits, int32_t dtype, int64_t N, int32_t E, 
   a.probs = out_probs;
   a.counts = out_counts;
   a.counted = out_rows;
-  rtopk::BalanceLayout l = rtopk::balance_layout(groups, a.per, E, dtype, k, true);
-  if (l.per_group > 1 && (!workspace || workspace_bytes < rtopk::balance_workspace(groups, E, l))) l = rtopk::balance_layout(groups, a.per, E, dtype, k, false);
+  const rtopk::RouterLanes lanes = rtopk::router_lanes(E, dtype, k, false);
+  rtopk::BalanceLayout l = rtopk::balance_layout(groups, a.per, lanes, true);
+  if (l.per_group > 1 && (!workspace || workspace_bytes < rtopk::balance_workspace(groups, E, l))) l = rtopk::balance_layout(groups, a.per, lanes, false);
   a.rows = l.rows;
   a.per_group = l.per_group;
   const int64_t parts = (int64_t)groups * l.per_group;
@@ -111,7 +112,7 @@ int rtopk_balance_loss_backward(const float* grad_loss, const float* grad_z, con
   a.counted_in = rows;
   a.grad_x = grad_logits;
   a.grad_stride = grad_stride;
-  const rtopk::BalanceLayout l = rtopk::balance_layout(groups, a.per, E, dtype, k, true);
+  const rtopk::BalanceLayout l = rtopk::balance_layout(groups, a.per, rtopk::router_lanes(E, dtype, k, true), true);
   a.rows = l.rows;
   a.per_group = l.per_group;
   return rtopk::launch_balance_grad(dtype, a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTOPK_OK : RTOPK_ERR_LAUNCH;

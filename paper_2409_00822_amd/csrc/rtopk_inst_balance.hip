@@ -7,7 +7,7 @@ namespace {
 
 template <int DT>
 hipError_t balance_of_type(const BalanceArgs& a, hipStream_t s) {
-  const RouterLanes r = router_lanes(a.E, DT, a.k);
+  const RouterLanes r = router_lanes(a.E, DT, a.k, false);
   const dim3 grid((uint32_t)(a.groups * a.per_group)), block(64 * kBalanceWaves);
 #define X(n, l)                                                                                           \
   if constexpr (is_router_of(DT, l))                                                                      \

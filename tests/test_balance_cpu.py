@@ -72,25 +72,27 @@ int main() {
     for (int E = 1; E <= kMaxExperts; ++E)
       for (int k : ks) {
         if (k > E) continue;
-        const RouterLanes r = router_lanes(E, dtype, k);
-        const int v = dtype == 0 ? 4 : 8;
-        if (r.lanes < 1 || r.lanes > 64 || (r.lanes & (r.lanes - 1)) || r.lanes * r.loads * v < E) ++bad;
-        if (E % v == 0 ? (r.lanes * r.loads - r.lanes) * v >= E && r.loads > 1 && r.lanes > 1 && r.lanes * v >= E : false) ++bad;  // no load that all lanes lack
-        bool compiled = false;
+        for (int grad = 0; grad < 2; ++grad) {
+          const RouterLanes r = router_lanes(E, dtype, k, grad);
+          const int v = dtype == 0 ? 4 : 8;
+          if (r.lanes < 1 || r.lanes > 64 || (r.lanes & (r.lanes - 1)) || r.lanes * r.loads * v < E) ++bad;
+          if (E % v == 0 ? (r.lanes * r.loads - r.lanes) * v >= E && r.loads > 1 && r.lanes > 1 && r.lanes * v >= E : false) ++bad;  // no load that all lanes lack
+          bool compiled = false;
 #define X(n, l) compiled |= r.lanes == n && r.loads == l && is_router_of(dtype, l);
-        RTOPK_ROUTER_LIST(X)
+          RTOPK_ROUTER_LIST(X)
 #undef X
-        if (!compiled) ++bad;
-        for (int64_t per : pers)
-          for (int64_t groups : counts)
-            for (int spread = 0; spread < 2; ++spread) {
-              const BalanceLayout l = balance_layout(groups, per, E, dtype, k, spread);
-              ++all;
-              // every token in one workgroup, none empty unless the group is
-              if (l.per_group < 1 || l.rows * l.per_group < per || (l.per_group > 1 && l.rows * (l.per_group - 1) >= per)) ++bad;
-              if (!spread && l.per_group != 1) ++bad;
-              if (groups * l.per_group > ((int64_t)1 << 23)) ++bad;  // 2^31 threads
-            }
+          if (!compiled) ++bad;
+          for (int64_t per : pers)
+            for (int64_t groups : counts)
+              for (int spread = 0; spread < 2; ++spread) {
+                const BalanceLayout l = balance_layout(groups, per, r, spread);
+                ++all;
+                // every token in one workgroup, none empty unless the group is
+                if (l.per_group < 1 || l.rows * l.per_group < per || (l.per_group > 1 && l.rows * (l.per_group - 1) >= per)) ++bad;
+                if (!spread && l.per_group != 1) ++bad;
+                if (groups * l.per_group > ((int64_t)1 << 23)) ++bad;  // 2^31 threads
+              }
+        }
       }
   printf("%ld %ld\n", bad, all);
   return bad != 0;
