@@ -8,8 +8,9 @@
 // therefore 64-bit here: their errors, 10^-13 of a row's mass, move one draw in 10^7 of a vocabulary of 131072 columns, where fp32 sums would move one in
 // a hundred.  That also spares the maximum: in 64 bits r = 0 does for all rows whose sum lies within 2^+-500, which is looked at afterwards.
 //
-// Bound by the vector ALU: a logit is sixteen 64-bit instructions, of 4.3 to 5 cycles each for 64 of them on a SIMD, 80 cycles in all, where HBM brings
-// 128 bytes in 48.
+// Bound by the vector ALU: 64 logits are 17 instructions, most of them 64-bit, of 5 cycles each on a SIMD, and three more for a piece's start and end: 100 cycles, where HBM
+// brings the 128 bytes in 48.  Slower: powers of bfloat16 logits from tables in LDS (43 us against 52 before the sums, but 64-bit reads keep a compute unit's LDS
+// busy for 26 cycles each, and with what corrects 32-bit ones 63), pieces of 2 or 8 loads of a wavefront (93 and 101 us against 87 with 4, 2047 x 50001 half).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -604,6 +605,9 @@ __device__ __forceinline__ int tested_up_to(const DrawArgs& a, int64_t n, int mo
   return most;
 }
 
+// 268 MB of bfloat16 logits by 512 workgroups 42 us (6.4 TB/s, vector ALU 69 %); 84 MB by 160 of 16 wavefronts 18 (160 of 256 compute units, whose ALUs are what is
+// waited for).  256 sequences of seven drafts in phases of two, two and three positions 117 us; of three and four 111, but where fewer drafts are accepted that
+// reads more rows for nothing.
 // Tests positions [pos0, pos0 + positions) of the sequences whose drafts before that have been accepted, a workgroup to each: most rows are read once, in fp32, at
 // the rate of HBM, and those behind a rejected draft not at all.
 template <int DT, int W>
@@ -659,7 +663,8 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
 __device__ __forceinline__ int rows_of(const DrawArgs& a) { return a.draft ? 2 * a.G + 1 : a.G + 1; }
 
 // The masses of pieces of a row (at temperature 0: their best columns) to scratch memory, a piece to a wavefront.  All rows that may be looked at, those behind a
-// rejected draft among them: few sequences leave the GPU room for that.
+// rejected draft among them: few sequences leave the GPU room for that.  2047 x 50001 half: 71 us, 2.9 TB/s, vector ALU busy 96 % of the time (640
+// instructions to a wavefront of 2048 columns); 64 x 131072 bfloat16 9.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) {
   const uint32_t rows = (uint32_t)rows_of(a);
@@ -685,7 +690,8 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_mass_kernel(DrawArgs a) 
   if (lane == 0) a.part[(n * rows + row) * a.pieces + piece] = out;
 }
 
-// The draws of sequences without drafts from their masses.
+// The draws of sequences without drafts from their masses, a chain of three loads: 3.2 us for one row, 9.8 for 2047.  By the kernel for drafts, with a third more
+// registers and loads twice, 5.6 and 15.6; with sixteen wavefronts one in six longer.
 template <int DT, int W>
 __global__ __launch_bounds__(64 * W) void draw_take_kernel(DrawArgs a) {
   __shared__ FindRoom<W> room;
@@ -715,7 +721,7 @@ __global__ __launch_bounds__(64 * W) void draw_take_kernel(DrawArgs a) {
   }
 }
 
-// Joins the masses, finds the first rejected draft and draws.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
+// Joins the masses, finds the first rejected draft and draws: a chain of some eight loads, 11 us for one sequence of four drafts, 32000 columns fp32.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
 // last one of them that is done (counted from 0, which draw_mass_kernel set) goes on; else the first one does it alone.  Which one is last changes
 // nothing: sums lie in memory and are taken in order.
 template <int DT, int W>
@@ -910,6 +916,8 @@ __device__ __forceinline__ double near_ratio(const DrawArgs& a, int64_t n, int p
   return (double)p.y / (double)q.y * power2(((double)p.x - (double)q.x) * c);
 }
 
+// 256 sequences, rows of 131072 bfloat16 columns: 62 us, 43 instructions to 64 pairs of columns, vector ALU 92 % busy.  (Sums first and what is left of p - q in a second
+// launch: 226 us for the whole call, and 177 so.)
 // The pieces of the row that a sequence draws from, one to a wavefront: its mass, and that of the draft's row and what is left of p - q where a draft was rejected.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) {
@@ -937,7 +945,7 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_rest_kernel(DrawArgs a) 
   }
 }
 
-// The draw of a sequence from those.
+// The draw of a sequence from those: a chain of loads, 8 us for 32 to 256 sequences.
 template <int DT>
 __global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) {
   using elem = typename Logits<DT>::elem;
