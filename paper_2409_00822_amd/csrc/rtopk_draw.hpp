@@ -721,7 +721,8 @@ __global__ __launch_bounds__(64 * W) void draw_take_kernel(DrawArgs a) {
   }
 }
 
-// Joins the masses, finds the first rejected draft and draws: a chain of some eight loads, 11 us for one sequence of four drafts, 32000 columns fp32.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
+// Joins the masses, finds the first rejected draft and draws: a chain of some eight loads, 11 us for one sequence of four drafts, 32000
+// columns fp32.  Where the draw is from max(p - q, 0) the sequence's workgroups take its pieces' sums, and the
 // last one of them that is done (counted from 0, which draw_mass_kernel set) goes on; else the first one does it alone.  Which one is last changes
 // nothing: sums lie in memory and are taken in order.
 template <int DT, int W>
@@ -740,7 +741,7 @@ __global__ __launch_bounds__(64 * W) void draw_join_kernel(DrawArgs a) {
     if (group == 0) write_sequence(a, n, 0, -1, T);
     return;
   }
-  const int g = a.G > 0 ? drafts_of(a, n) : 0;
+  const int g = drafts_of(a, n);
   const double2* parts = a.part + n * rows * a.pieces;
   if (heat.certain()) {
     if (group != 0) return;
@@ -1019,7 +1020,9 @@ __global__ __launch_bounds__(64 * kDrawWaves) void draw_pick_kernel(DrawArgs a) 
   }
   int drawn = -1;
   if (w.is_number())
-    drawn = block_draw<DT, W>(a, w, p, q, [&](int j) { return part[j]; }, [&](int j) { return fmax(__builtin_fma(-more, rest[j].y, rest[j].x), 0.0) * w.over_p; }, (double)a.uniforms[n * (a.G + 1) + a.G], room);
+    drawn = block_draw<DT, W>(
+        a, w, p, q, [&](int j) { return part[j]; }, [&](int j) { return fmax(__builtin_fma(-more, rest[j].y, rest[j].x), 0.0) * w.over_p; },
+        (double)a.uniforms[n * (a.G + 1) + a.G], room);
   write_sequence(a, n, pos, drawn, T);
 }
 
