@@ -270,6 +270,27 @@ def test_in_the_logits_place(dtype, E):
     assert torch.isnan(whole[:-1, E:]).all()  # what lies between rows is left as it was
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("E,bytes", [(7, 4), (33, 1), (96, 4), (256, 1), (523, 4)])
+def test_given_outputs_and_what_lies_between_rows(dtype, E, bytes):
+    R = _gpu()
+    N, k, groups = 90, min(E, 5), 3
+    x, cols = inputs(N, E, k, dtype, E, 5, 1, 4, bytes) if bytes == 4 else inputs(N, E, k, dtype, E, 5, 1, 0, bytes)
+    if E == 256:
+        cols[:, k - 1] = 255
+    out = [torch.full(s, 7, dtype=t, device="cuda") for s, t in (((groups,), torch.float32),) * 2 + (((groups, E), torch.float32), ((groups, E), torch.int32), ((groups,), torch.int32))]
+    got = R.rtopk_balance_loss(x, cols, groups, *out)
+    assert all(a.data_ptr() == b.data_ptr() for a, b in zip(got, out))
+    check_forward(R, x, cols, groups, got)
+    gl, gz, gv = upstream(groups, N, k, dtype, 3)
+    buf = torch.full((N * (E + 3) + 9,), 5.0, dtype=TYPES[dtype], device="cuda")
+    to = buf[1:1 + N * (E + 3)].view(N, E + 3)
+    for more in ((), (gz, gv)):
+        buf.fill_(5.0)
+        grad = check_gradient(R, x, cols, got[3], got[4], gl, *more, grad_logits=to[:, :E])
+        assert grad.data_ptr() == to.data_ptr() and (to[:, E:] == 5).all() and buf[0] == 5 and (buf[1 + N * (E + 3):] == 5).all()
+
+
 def test_against_differences():
     R = _gpu()
     x, cols = inputs(24, 10, 2, "f32", 6, scale=1.0)

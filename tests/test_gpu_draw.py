@@ -324,6 +324,18 @@ def test_the_widest_rows(dtype, B, G, M):
     assert status == 0 and torch.equal(out, want[0]) and torch.equal(n, want[1])
 
 
+@pytest.mark.parametrize("N,M", [(5, 700), (3, 40000), (600, 9000)])
+def test_tokens_of_32_bits_and_what_lies_around_them(N, M):
+    R = _gpu()
+    x, u = block((N, M), "bf16", 5, pad=3, shift=1), numbers((N,), 6)
+    buf = torch.full((N + 2,), 77, dtype=torch.int32, device="cuda")
+    got = R.rtopk_sample_tokens(x, u, 0.9, out_tokens=buf[1:N + 1])
+    assert got.data_ptr() == buf[1:].data_ptr() and buf[0] == 77 and buf[N + 1] == 77
+    assert torch.equal(got.long(), R.rtopk_sample_tokens(x, u, 0.9))
+    some = slice(0, 5)
+    check_sample(R, x[some], u[some], 0.9)
+
+
 def test_captured_and_on_other_streams():
     R = _gpu()
     B, G, M = 4, 3, 32000
