@@ -292,8 +292,8 @@ int rtopk_distill_with_grad(const float* weights, const void* logits, int32_t dt
  *                  temperature is negative, infinite or NaN gets no token (-1) and no draft accepted.
  *   temperature  : 0, or finite and positive with a finite reciprocal (RTOPK_ERR_BAD_TEMPERATURE); not looked at where temperatures is given.
  *   token_bytes  : of drafts and out_tokens, 4 (int32_t) or 8 (int64_t).
- *   workspace    : as above, rtopk_verify_workspace_bytes(...) bytes (for rtopk_sample_tokens with G and draft_logits 0): few sequences are then spread
- *                  over many workgroups, in a few launches.  Drawn tokens of both ways can differ only where u lies within rounding, about 1e-13, of a border.
+ *   workspace    : as above, rtopk_verify_workspace_bytes(...) bytes, which do for any temperature (for rtopk_sample_tokens with G and draft_logits 0): few
+ *                  sequences are then spread over many workgroups, in a few launches.  Drawn tokens of both ways can differ only where u lies within rounding, about 1e-13, of a border.
  */
 int64_t rtopk_verify_workspace_bytes(int64_t B, int32_t G, int32_t M, int32_t dtype, int32_t draft_logits);
 

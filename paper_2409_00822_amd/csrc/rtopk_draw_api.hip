@@ -30,8 +30,9 @@ extern "C" {
 
 int64_t rtopk_verify_workspace_bytes(int64_t B, int32_t G, int32_t M, int32_t dtype, int32_t draft_logits) {
   if (B < 1 || G < 0 || G > rtopk::kMaxDrafts || M < 1 || M > rtopk::kMaxLogitsM || !is_type(dtype) || (draft_logits & ~1) != 0) return 0;
-  const bool draft = draft_logits != 0 && G > 0;
-  return rtopk::draw_workspace(B, G, draft, rtopk::draw_layout(B, G, M, dtype, draft));
+  const auto need = [&](bool draft) { return rtopk::draw_workspace(B, G, draft, rtopk::draw_layout(B, G, M, dtype, draft)); };
+  const int64_t without = need(false), with = draft_logits != 0 && G > 0 ? need(true) : 0;
+  return without > with ? without : with;  // (a call at temperature 0 is laid out without its draft logits)
 }
 
 int rtopk_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype, int64_t B, int32_t G, int32_t M, int64_t target_seq_stride,
