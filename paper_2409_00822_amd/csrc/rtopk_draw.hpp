@@ -590,11 +590,6 @@ __global__ __launch_bounds__(64 * W) void draw_kernel(DrawArgs a) {
 
 // ---- drafts tested beforehand ----------------------------------------------------------------------
 
-// fp32 sums of a row are off by less than 512 units of 2^-24: of up to 2^20 columns 256 threads add up to 256 batches each, one behind the other, of 16 terms
-// to an accumulator, and terms that weigh are off by some tens of units each.  Where u q and p are nearer to each other than two rows' errors, they are computed again
-// in 64 bits.
-constexpr double kTestMargin = 0x1p-14;
-
 // The first of `most` positions whose draft the tests have rejected; each wavefront for itself.
 __device__ __forceinline__ int tested_up_to(const DrawArgs& a, int64_t n, int most) {
   const int lane = threadIdx.x & 63;
@@ -631,16 +626,18 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
   } else {
     const double u = (double)a.uniforms[n * (a.G + 1) + pos];
     const float c = (float)heat.c;
+    double margin = kTestMargin;
     const auto near = [&](const elem* x, int which) {
-      const Segment<DT> g(x, a.M);  // (eight loads at a time for a workgroup of sixteen, which has no other beside it)
-      const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, W == 16 ? 8 : 4, false, false>(g, c), c, sums);
+      const Segment<DT> g(x, a.M);
+      const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, test_loads(W), false, false>(g, c), c, sums);
       __syncthreads();
+      if (far_maximum(t.m, c)) margin = kFarTestMargin;
       if (threadIdx.x == 0) a.near[2 * (n * a.G + pos) + which] = make_float2(t.m, t.s);
       return power2(((double)Logits<DT>::widen(x[d]) - (double)t.m) * heat.c) / (double)t.s;
     };
     double p_d = near(p, 0), uq = a.draft ? u * near(q, 1) : u;
-    accepted = uq < p_d * (1.0 - kTestMargin);
-    if (!accepted && !(uq > p_d * (1.0 + kTestMargin))) {
+    accepted = uq < p_d * (1.0 - margin);
+    if (!accepted && !(uq > p_d * (1.0 + margin))) {  // (nearer than the sums are exact: again, in 64 bits)
       const auto exact = [&](const elem* x) {
         const Mass t = piece_mass<DT>(x + first, mine, lane, heat.c);
         __syncthreads();
