@@ -131,23 +131,23 @@ template <int DT>
 __device__ __forceinline__ Mass piece_mass(const typename Logits<DT>::elem* piece, int cols, int lane, double c) {
   using L = Logits<DT>;
   constexpr int U = DT == kF32 ? 4 : 2;
-  const int full = cols / L::V, rest = cols % L::V;
   double s = 0.0;
   bool masked = false;
-  int i = lane;
-  for (; i - lane + U * 64 <= full; i += U * 64) {
-    u4_vec w[U];
+  lane_of_piece<L::V, U>(
+      cols, lane,
+      [&](int i) {
+        u4_vec w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = L::load(piece + (uint32_t)(i + u * 64) * L::V);
-    s += chunk_powers<DT, U>(w, c, masked);
-  }
-  for (; i - lane < full; i += 64) {
-    u4_vec w[1] = {u4_vec{L::kLow, L::kLow, L::kLow, L::kLow}};
-    if (i < full) w[0] = L::load(piece + (uint32_t)i * L::V);
-    masked |= i - lane + 64 > full;
-    s += chunk_powers<DT, 1>(w, c, masked);
-  }
-  if (lane < rest) s += masked_power(L::widen(piece[full * L::V + lane]), c);
+        for (int u = 0; u < U; ++u) w[u] = L::load(piece + (uint32_t)(i + u * 64) * L::V);
+        s += chunk_powers<DT, U>(w, c, masked);
+      },
+      [&](int i, bool is, bool some) {
+        u4_vec w[1] = {u4_vec{L::kLow, L::kLow, L::kLow, L::kLow}};
+        if (is) w[0] = L::load(piece + (uint32_t)i * L::V);
+        masked |= some;
+        s += chunk_powers<DT, 1>(w, c, masked);
+      },
+      [&](int col) { s += masked_power(L::widen(piece[col]), c); });
   Mass t = {0.0, wave_sum(s)};
   if (!(t.s >= kLeastSum && t.s <= kMostSum)) {  // about the maximum then
     float m = kNegInf;
@@ -846,7 +846,6 @@ template <int DT>
 __device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, const typename Logits<DT>::elem* q, int cols, int lane, double c, double ratio) {
   using L = Logits<DT>;
   Rest r = {0.0, 0.0, 0.0, 0.0, __builtin_inf()};
-  const int full = cols / L::V, rest = cols % L::V;
   const double near = ratio * kNear;
   bool masked = false;
   const auto add = [&](double ep, double eq, Rest& t, bool& close) {
@@ -861,46 +860,48 @@ __device__ __forceinline__ Rest piece_rest(const typename Logits<DT>::elem* p, c
     const double eq = masked_power(y, c), d = __builtin_fma(-ratio, eq, masked_power(x, c));
     if (fabs(d) < near * eq) r.nearest = fmin(r.nearest, fabs(d) / eq);
   };
-  for (int i = lane; i - lane < full; i += 64) {
-    Rest t = {0.0, 0.0, 0.0, 0.0, 0.0};
-    bool close = false;
-    u4_vec x[1], y[1];
-    if (i < full) {
-      x[0] = L::load(p + (int64_t)i * L::V);
-      y[0] = L::load(q + (int64_t)i * L::V);
-      if (!masked) {
+  lane_of_piece<L::V, 1>(
+      cols, lane, [](int) {},
+      [&](int i, bool is, bool) {
+        Rest t = {0.0, 0.0, 0.0, 0.0, 0.0};
+        bool close = false;
+        u4_vec x[1], y[1];
+        if (is) {
+          x[0] = L::load(p + (int64_t)i * L::V);
+          y[0] = L::load(q + (int64_t)i * L::V);
+          if (!masked) {
 #pragma unroll
-        for (int k = 0; k < L::V; ++k) add(power2_finite((double)L::at(x[0], k) * c), power2_finite((double)L::at(y[0], k) * c), t, close);
-      }
-    }
-    if (masked || __any(!(t.p + t.q == t.p + t.q))) {  // (-inf, or what is no number)
-      masked = true;
-      close = false;
-      t = {0.0, 0.0, 0.0, 0.0, 0.0};
-      if (i < full) {
-        apart(x);
-        apart(y);
+            for (int k = 0; k < L::V; ++k) add(power2_finite((double)L::at(x[0], k) * c), power2_finite((double)L::at(y[0], k) * c), t, close);
+          }
+        }
+        if (masked || __any(!(t.p + t.q == t.p + t.q))) {  // (-inf, or what is no number)
+          masked = true;
+          close = false;
+          t = {0.0, 0.0, 0.0, 0.0, 0.0};
+          if (is) {
+            apart(x);
+            apart(y);
 #pragma unroll
-        for (int k = 0; k < L::V; ++k) add(masked_power(L::at(x[0], k), c), masked_power(L::at(y[0], k), c), t, close);
-      }
-    }
-    r.p += t.p;
-    r.q += t.q;
-    r.a += t.a;
-    r.b += t.b;
-    if (__any(close)) {  // (seldom)
-      if (close) {
+            for (int k = 0; k < L::V; ++k) add(masked_power(L::at(x[0], k), c), masked_power(L::at(y[0], k), c), t, close);
+          }
+        }
+        r.p += t.p;
+        r.q += t.q;
+        r.a += t.a;
+        r.b += t.b;
+        if (__any(close)) {  // (seldom)
+          if (close) {
 #pragma unroll 1
-        for (int k = 0; k < L::V; ++k) approach(L::widen(p[(int64_t)i * L::V + k]), L::widen(q[(int64_t)i * L::V + k]));
-      }
-    }
-  }
-  if (lane < rest) {
-    const float x = L::widen(p[full * L::V + lane]), y = L::widen(q[full * L::V + lane]);
-    bool close = false;
-    add(masked_power(x, c), masked_power(y, c), r, close);
-    approach(x, y);
-  }
+            for (int k = 0; k < L::V; ++k) approach(L::widen(p[(int64_t)i * L::V + k]), L::widen(q[(int64_t)i * L::V + k]));
+          }
+        }
+      },
+      [&](int col) {
+        const float x = L::widen(p[col]), y = L::widen(q[col]);
+        bool close = false;
+        add(masked_power(x, c), masked_power(y, c), r, close);
+        approach(x, y);
+      });
   if (__any(r.nearest < __builtin_inf())) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) r.nearest = fmin(r.nearest, __shfl_xor(r.nearest, d));

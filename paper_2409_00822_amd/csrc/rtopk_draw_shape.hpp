@@ -36,6 +36,19 @@ inline DrawLayout draw_pieces(int M, int dtype, int64_t loads, int most) {
   return {false, 4, (int)ceil_div(M, loads * step), (int)(loads * step), 1, false, 0, 0};
 }
 
+// What lane `lane` of a wavefront reads of a piece of `cols` columns, in loads of V of them: batch(i) for U chunks from i on, 64 apart, while all lanes have U; then
+// one(i, is, some) for chunk i, which there `is` for this lane or not; `some`: not for all of them; and rest(c) for a column of what is less than a chunk.
+template <int V, int U, typename Batch, typename One, typename Rest>
+__attribute__((always_inline)) constexpr void lane_of_piece(int cols, int lane, Batch batch, One one, Rest rest) {
+  const int full = cols / V;
+  int i = lane;
+  if constexpr (U > 1) {
+    for (; i - lane + U * 64 <= full; i += U * 64) batch(i);
+  }
+  for (; i - lane < full; i += 64) one(i, i < full, i - lane + 64 > full);
+  if (lane < cols % V) rest(full * V + lane);
+}
+
 // One wavefront to a short sequence where there are many, which pays no barriers (tokens of 16384 rows of 1000 bfloat16 logits 41 us, with four 94; 1024 rows
 // 7.4 and 8.7, 64 rows 6.7 and 6.5; 4096 x 8000 43 and 49, 1024 x 8000 21 and 16); else four for short rows or many, eight for few of up to 8192
 // columns, sixteen for few wide ones.
