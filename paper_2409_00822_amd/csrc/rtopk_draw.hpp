@@ -626,16 +626,17 @@ __global__ __launch_bounds__(64 * W) void draw_test_kernel(DrawArgs a, int pos0,
   } else {
     const double u = (double)a.uniforms[n * (a.G + 1) + pos];
     const float c = (float)heat.c;
-    double margin = kTestMargin;
+    int64_t units = 0;
     const auto near = [&](const elem* x, int which) {
       const Segment<DT> g(x, a.M);
       const Stats t = segment_stats<DT, W, false>(g, thread_stats<DT, T, test_loads(W), false, false>(g, c), c, sums);
       __syncthreads();
-      if (far_maximum(t.m, c)) margin = kFarTestMargin;
+      units += test_units(a.M, DT, W, far_maximum(t.m, c));
       if (threadIdx.x == 0) a.near[2 * (n * a.G + pos) + which] = make_float2(t.m, t.s);
       return power2(((double)Logits<DT>::widen(x[d]) - (double)t.m) * heat.c) / (double)t.s;
     };
     double p_d = near(p, 0), uq = a.draft ? u * near(q, 1) : u;
+    const double margin = test_margin(units);
     accepted = uq < p_d * (1.0 - margin);
     if (!accepted && !(uq > p_d * (1.0 + margin))) {  // (nearer than the sums are exact: again, in 64 bits)
       const auto exact = [&](const elem* x) {

@@ -85,18 +85,22 @@ constexpr int test_loads(int waves) { return waves == 16 ? 8 : 4; }
 // Units of 2^-24 of its value that the fp32 sum of a row of M columns about its maximum is off by at most when drafts are tested; far: where maximum / T is beyond
 // what sums run along with (far_maximum), so that each term is taken from the maximum itself.  Terms are weighed by what they are of the sum, and by that their
 // distances t from the maximum, in powers of two, average to no more than log2 M <= 20 (an entropy less the log of a sum that is 1 or more):
-//   each term   the factor log2(e) / T and the exponent rounded, 2 ln 2 t = 28 (far: the difference too, 42); exp2 2; a factor without all its bits (T > 10^38) 6
+//   each term   the factor log2(e) / T and the exponent rounded, 2 ln 2 t = 28 (far: the difference too, 42); exp2 2 (off by 0.79 units of its last place at
+//               most, over all arguments); a factor without all its bits (T > 10^38) 6
 //   each batch  near: half its terms to an accumulator, their sum to the thread's 1, scaled before by an exp2, which is off by 1 + its distance, and a product 1
 //               (what it is scaled by is 1, exactly, unless the maximum has risen); far: one term behind the other
 //   distances that sums are scaled over, 20; two joins of 6 additions, each scaled by 2; from the sums' reference to the maximum 4.  Far: joins of 6 and 16.
-inline int64_t test_units(int M, int dtype, int waves, bool far) {
+constexpr int64_t test_units(int M, int dtype, int waves, bool far) {
   const int64_t width = logits_width(dtype), threads = 64 * waves, loads = test_loads(waves), chunks = M / width + 2;
-  if (far) return (chunks + threads - 1) / threads * width + 42 + 2 + 6 + 6 + 16;
-  return 3 * (chunks / (threads * loads) + loads + 1) + loads * width / 2 + 28 + 2 + 6 + 20 + 2 * (6 + 2) + 4;
+  return far ? (chunks + threads - 1) / threads * width + 42 + 2 + 6 + 16 : 3 * (chunks / (threads * loads) + loads + 1) + loads * width / 2 + 28 + 2 + 6 + 20 + 2 * (6 + 2) + 4;
 }
 
-// A draft is decided on in fp32 where u q and p are farther from each other, relative to p, than both rows' sums may be off.
-constexpr double kTestMargin = 0x1p-13, kFarTestMargin = 0x1p-10;
+// A draft is decided on in fp32 where u q and p are farther from each other, relative to p, than both rows' sums may be off; units: of both.  (Roundings behind one another
+// and quotients of them add terms of the second order, less than four squares.)  Wider margins cost time, as a draft that is nearer takes its row's workgroup 20 us more.
+constexpr double test_margin(int64_t units) {
+  const double off = (double)units * 0x1p-24;
+  return off + 4.0 * off * off;
+}
 
 inline DrawLayout draw_layout(int64_t B, int G, int M, int dtype, bool draft) {
   if (by_workgroups(B, G, M)) return draw_layout_whole(B, M, dtype);
