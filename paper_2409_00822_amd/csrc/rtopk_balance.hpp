@@ -10,7 +10,7 @@
 // its columns' probabilities over the tokens it sees, in fp32 for kFlush turns and in 64 bits over lanes and (LDS) over these; picks are counted by integer atomics
 // in LDS, whose order changes nothing.  Workgroups leave their sums in scratch memory and a second kernel joins them in order.
 //
-// Bound by HBM and the vector ALU alike: 262144 x 256 bfloat16 30 us (4.7 TB/s, ALU 86 % busy) and 4.5 for the join; gradient 1048576 x 128 bfloat16 with picked
+// Bound by HBM and the vector ALU alike: 262144 x 256 bfloat16 28 to 29 us (5.0 TB/s, ALU 84 % busy) and 4.6 for the join; gradient 1048576 x 128 bfloat16 with picked
 // values 109 us (603 MB, 5.5 TB/s, ALU 62 %).  Four tokens' loads in flight and moved columns out of the loads' way took the gradient from 315 us to
 // 136, sums of lanes by one instruction a step to 117, two loads to a lane to 108.
 #pragma once

@@ -600,7 +600,7 @@ __device__ __forceinline__ int tested_up_to(const DrawArgs& a, int64_t n, int mo
   return most;
 }
 
-// 268 MB of bfloat16 logits by 512 workgroups 42 us (6.4 TB/s, vector ALU 69 %); 84 MB by 160 of 16 wavefronts 18 (160 of 256 compute units, whose ALUs are what is
+// 269 MB of bfloat16 logits by 512 workgroups 42 us (6.4 TB/s, vector ALU 67 %); 84 MB by 160 of 16 wavefronts 18 (160 of 256 compute units, whose ALUs are what is
 // waited for).  256 sequences of seven drafts in phases of two, two and three positions 117 us; of three and four 111, but where fewer drafts are accepted that
 // reads more rows for nothing.
 // Tests positions [pos0, pos0 + positions) of the sequences whose drafts before that have been accepted, a workgroup to each: most rows are read once, in fp32, at
@@ -916,7 +916,7 @@ __device__ __forceinline__ double near_ratio(const DrawArgs& a, int64_t n, int p
   return (double)p.y / (double)q.y * power2(((double)p.x - (double)q.x) * c);
 }
 
-// 256 sequences, rows of 131072 bfloat16 columns: 62 us, 43 instructions to 64 pairs of columns, vector ALU 92 % busy.  (Sums first and what is left of p - q in a second
+// 256 sequences, rows of 131072 bfloat16 columns: 61 to 62 us, 43 instructions to 64 pairs of columns, vector ALU 92 % busy.  (Sums first and what is left of p - q in a second
 // launch: 226 us for the whole call, and 177 so.)
 // The pieces of the row that a sequence draws from, one to a wavefront: its mass, and that of the draft's row and what is left of p - q where a draft was rejected.
 template <int DT>

@@ -73,7 +73,9 @@ inline bool by_workgroups(int64_t B, int G, int M) {
 // Drafts tested beforehand, us against all rows' sums in 64 bits, four drafts: bfloat16, 32000 columns 16 sequences 20.5 and 17.4, 32 21.3 and 21.8, 64 24.5 and 28.0, 256 53.7
 // and 70.9; 131072 columns 16 sequences 37.8 and 29.3, 32 39.1 and 44.3, 64 47.7 and 71.8, 256 131 and 260; fp32, 32000 columns 32 sequences 24.7 and 21.0, 128 40.9 and
 // 46.1, 131072 columns 16 sequences 47.0 and 32.5, 64 69.5 and 91.0.  A workgroup to a row is slow for few wide rows.  Narrower rows only where they are
-// many (8000 columns, eight drafts, 256 sequences 48.4 and 40.3; 4000 columns, four drafts, 4096 sequences 135 and 178).
+// many (8000 columns, eight drafts, 256 sequences 48.4 and 40.3; 4000 columns, four drafts, 4096 sequences 135 and 178).  Those are of drafts with logits; drafts that were
+// looked up, on both sides of the same line (tested, with one sequence fewer not): 131072 columns, seven drafts, 32 sequences 24.8 and 32, three drafts, 64 27.1 and 31.5;
+// 50001 half 19.5 and 18.8; 32000, three drafts, 66 16.3 and 16.4, seven drafts, 33 15.4 and 15.9.
 inline bool test_first(int64_t B, int G, int M, int dtype, bool draft) {
   const int64_t cells = B * draw_rows(G, draft) * M, least = (int64_t)256 * M;
   return G > 0 && M <= kMostTested && (M >= 16384 || B >= 1024) && cells >= (least > (1 << 23) ? least : 1 << 23) + (dtype == 0 ? 1 << 23 : 0);
